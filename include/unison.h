@@ -418,6 +418,158 @@ int unison_debug_cache_slots(unison_ctx* ctx, int slots);
  * take. */
 int unison_debug_kendall_barrier(uint32_t n_pad, uint32_t step, uint32_t a, uint32_t b);
 
+/* ------------------------------------------------ the KV inside the sessions
+ * (C ABI without a context; arrays DEVICE and 16-byte aligned unless stated;
+ * asynchronous on `hip_stream`, which belongs to the current device).
+ *
+ * The pool's residency policies decide which sessions stay.  These operators
+ * work on the entries of the sessions that did: a turn's new tokens go into
+ * pages (unison_kv_append), attend over their session while every entry's
+ * accumulated attention weight is kept (unison_kv_attend), or over the pages
+ * that a cheap integer score selects (unison_kv_attend_blocks), and the
+ * entries of least weight leave a session that is over its budget
+ * (unison_kv_victims, unison_kv_compact).  All results are deterministic. */
+
+#define UNISON_KV_BF16 0u
+#define UNISON_KV_FP16 1u
+
+/* A pool of pages.  Keys of a page and kv head are rows [page][head_dim],
+ * values are transposed, [head_dim][page]. */
+typedef struct {
+  uint32_t dtype;    /* UNISON_KV_BF16 or UNISON_KV_FP16: q, k, v and out */
+  uint32_t head_dim; /* 64, 128 or 256 */
+  uint32_t n_kv;     /* kv heads, 1..1024 */
+  uint32_t page;     /* entries of a page: 16, 32, 64, 128 or 256 */
+  uint32_t n_pages;  /* 1..2^31 - 1 */
+  uint32_t pad0;
+  void* k;           /* [n_pages][n_kv][page][head_dim] */
+  void* v;           /* [n_pages][n_kv][head_dim][page] */
+  float* weight;     /* [n_pages][n_kv][page] accumulated attention weight, or NULL */
+  int32_t* pos;      /* [n_pages][n_kv][page] token position of an entry, or NULL */
+  int8_t* box;       /* [n_pages][n_kv][2][head_dim] lower and upper sides, or NULL */
+  float* box_scale;  /* [n_pages][n_kv] size of a box step; NULL exactly when box is */
+} unison_kv_pool;
+
+/* A batch of sequences over a pool.  Entry e of sequence s is slot e % page of
+ * page pages[s][e / page].  Its new tokens, rows tok[s] .. tok[s+1]-1 of the
+ * token arrays, are its last tok[s+1] - tok[s] entries: `len` counts them.
+ * A page id outside 0..n_pages-1 is a page that is not there: its entries are
+ * neither read nor written and no token sees them.  A length is taken as
+ * 0..max_len, token ranges are cut to n_tok rows and max_new tokens, so no
+ * content of these arrays leads outside the caller's memory.  Sequences may
+ * share pages in calls that do not write them (attention without weights). */
+typedef struct {
+  uint32_t n_seq;       /* 0..65535; 0: the call does nothing */
+  uint32_t max_pages;   /* page ids per sequence; max_pages * page <= 2^30 */
+  uint32_t n_tok;       /* rows of the token arrays */
+  uint32_t max_new;     /* no sequence has more new tokens; >= 1 if n_tok is */
+  uint32_t max_len;     /* no sequence is longer; 0: max_pages * page */
+  uint32_t pad0;
+  const int32_t* pages; /* [n_seq][max_pages], 4-byte aligned */
+  const int32_t* len;   /* [n_seq], 4-byte aligned */
+  const int32_t* tok;   /* [n_seq + 1], non-decreasing, 4-byte aligned (not read
+                           by unison_kv_victims and unison_kv_compact) */
+} unison_kv_seqs;
+
+/* Rows of the new tokens: element (token, head, d) is
+ * p[token * tok_stride + head * head_stride + d].  p is 16-byte aligned and
+ * the strides are multiples of 8 elements. */
+typedef struct {
+  const void* p;
+  uint64_t tok_stride, head_stride;
+} unison_kv_rows;
+
+/* Writes the new tokens' k and v rows ([n_tok][n_kv][head_dim]) into their
+ * entries, sets those entries' weights to 0 and their positions to
+ * tok_pos[token] where the pool has them, and renews the boxes of the pages
+ * that got entries: with A the largest magnitude of a page's live keys,
+ * 2^(e-1) <= A < 2^e, the step is 2^(e-7) and the box holds floor(min / step)
+ * and ceil(max / step) per dimension over the live keys, cut to -127..127
+ * (step and box 0 for A < 2^-120).  Keys are finite where boxes are kept.
+ * tok_pos: [n_tok], needed exactly when the pool has positions.
+ * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
+int unison_kv_append(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
+                     const unison_kv_rows* k, const unison_kv_rows* v, const int32_t* tok_pos);
+
+/* Workspace bytes of unison_kv_attend (weights: whether it keeps weights) and
+ * of unison_kv_attend_blocks (n_sel > 0).  Only the sizes of the structs are
+ * read.  Errors: UNISON_E_INVALID, UNISON_E_CAPACITY. */
+int unison_kv_attend_size(const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t n_q,
+                          int weights, uint32_t n_sel, size_t* bytes);
+
+/* Attention of the new tokens.  Token i of a sequence's n new ones sees its
+ * entries e < len - n + i + 1 (and no page that is not there).  Query head h
+ * reads kv head h / (n_q / n_kv).  s = scale q.k; out = sum p v with
+ * p = exp(s) / sum exp(s); lse = log sum exp(s).  A token that sees nothing
+ * gets out = 0 and lse = -inf.
+ * weights != 0: weight[e] = decay * weight[e] + the sum of p over the
+ * sequence's new tokens and the kv head's query heads, for every live entry of
+ * every sequence that has new tokens (its pages belong to it alone).
+ * Values of the live entries are finite: a new token's NaN may reach the other
+ * new tokens of its sequence.  Slots at and past `len` may hold anything.
+ * q, out: [n_tok][n_q][head_dim], out contiguous; lse: [n_tok][n_q] or NULL.
+ * Rows of `out` and `lse` that belong to no sequence are left as they were.
+ * workspace: at least unison_kv_attend_size() bytes, 256-byte aligned; its
+ * contents mean nothing before and after the call; calls that may overlap
+ * need workspaces of their own.
+ * Errors: UNISON_E_INVALID (also: weights without pool->weight, decay outside
+ * 0..1, scale not finite, n_q no multiple of n_kv, over 128 query heads a kv
+ * head, a short workspace), UNISON_E_CAPACITY, UNISON_E_HIP. */
+int unison_kv_attend(void* hip_stream, void* workspace, size_t workspace_bytes,
+                     const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t n_q,
+                     const unison_kv_rows* q, float scale, int weights, float decay, void* out,
+                     float* lse);
+
+/* The same over at most n_sel pages for each token and kv head.  The pages
+ * that a token sees are those of its visible entries.  Chosen are the first
+ * `first` and the last `last` of them and then, until there are n_sel, the
+ * ones of highest score, ties to the lower page:
+ *   score = step * sum over the kv head's query heads and dimensions of
+ *           max(qi * lower, qi * upper)
+ * with qi the query rounded to whole steps (half to even) of one power of two
+ * for the kv head's query heads, the largest magnitude in 64..127.  The sum is
+ * a whole number, so the choice does not depend on an order of summation.
+ * sel: [n_tok][n_kv][n_sel], the chosen ordinals ascending (pages[s][ordinal]),
+ * -1 behind the last; rows of no sequence are left as they were.
+ * 1 <= last, first + last <= n_sel <= 4096, max_pages <= 32768 (else
+ * UNISON_E_CAPACITY).  Needs the pool's boxes.  Weights are not kept.
+ * Otherwise as unison_kv_attend. */
+int unison_kv_attend_blocks(void* hip_stream, void* workspace, size_t workspace_bytes,
+                            const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t n_q,
+                            const unison_kv_rows* q, float scale, uint32_t n_sel, uint32_t first,
+                            uint32_t last, void* out, float* lse, int32_t* sel);
+
+/* Eviction by accumulated attention weight.  A sequence of more than `budget`
+ * entries loses n = min(len - budget, max_evict) of them in every kv head:
+ * those of least weight (NaN counts as 0), ties to the lower slot.  Entries
+ * whose position is below `first` or above the kv head's highest position
+ * minus `recent` go only when nothing else is left, lower slots first; so do
+ * entries of pages that are not there.
+ *   new_len [n_seq]              = len - n
+ *   victims [n_seq][n_kv][max_evict]  the n entries that go, ascending, then -1
+ *   src     [n_seq][n_kv][max_evict]  for each victim below new_len the entry
+ *                                that moves into its place: the kept entries at
+ *                                and past new_len, ascending; else -1
+ * Nothing in the pool changes.  Needs the pool's weights and positions;
+ * budget >= first + recent, budget >= 1, 1 <= max_evict <= 2^30.  The three
+ * arrays are 4-byte aligned.
+ * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
+int unison_kv_victims(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
+                      uint32_t budget, uint32_t first, uint32_t recent, uint32_t max_evict,
+                      int32_t* victims, int32_t* src, int32_t* new_len);
+
+/* Carries unison_kv_victims' lists out: entry src moves into its victim's
+ * place with its key, value, weight and position, and the boxes of every page
+ * that lost or got an entry are renewed over its entries below new_len.  `seqs`
+ * still has the old lengths; afterwards new_len takes their place.  Moves
+ * read at and past new_len and write below it, so their order does not matter
+ * and a second call with the same lists changes nothing.  A list entry
+ * outside that is no move.
+ * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
+int unison_kv_compact(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
+                      uint32_t max_evict, const int32_t* victims, const int32_t* src,
+                      const int32_t* new_len);
+
 uint32_t unison_version(void);
 
 #ifdef __cplusplus

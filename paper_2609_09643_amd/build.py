@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libunison.so")
-SOURCES = ["sim.hip", "lane.hip", "rank.hip", "api.cpp"]
+SOURCES = ["sim.hip", "lane.hip", "rank.hip", "api.cpp", "kv_cache.hip", "kv_attend.hip",
+           "kv_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

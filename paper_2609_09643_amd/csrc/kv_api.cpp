@@ -1,0 +1,188 @@
+// kv_api.cpp -- host side of the paged-KV operators (see include/unison.h): checks every size,
+// pointer and stride that the kernels rely on, then launches them on the caller's stream.
+#include <cmath>
+
+#include "kv_device.h"
+
+namespace unison {
+hipError_t launch_kv_append(const KvArgs& a, const KvRows& k, const KvRows& v, const int32_t* pos,
+                            hipStream_t st);
+hipError_t launch_kv_victims(const KvArgs& a, uint32_t budget, uint32_t first, uint32_t recent,
+                             uint32_t max_evict, int32_t* victims, int32_t* src, int32_t* new_len,
+                             hipStream_t st);
+hipError_t launch_kv_compact(const KvArgs& a, uint32_t max_evict, const int32_t* victims, const int32_t* src,
+                             const int32_t* new_len, hipStream_t st);
+size_t kv_attend_bytes(const KvArgs& a, bool weights, uint32_t n_sel);
+hipError_t launch_kv_attend(const KvArgs& a, const KvRows& q, float scale, bool weights, float decay,
+                            uint32_t n_sel, uint32_t first, uint32_t last, void* out, float* lse, int32_t* sel,
+                            void* ws, hipStream_t st);
+}  // namespace unison
+
+using namespace unison;
+
+namespace {
+
+constexpr uint32_t kMaxSeqs = 65535, kMaxKvHeads = 1024, kMaxGroup = 128, kMaxSelPages = 32768, kMaxSel = 4096;
+constexpr uint64_t kMaxEntries = 1ull << 30;
+
+bool on(const void* p, size_t bytes) { return p && reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// The sizes of a pool and a batch; no pointer is looked at.
+int sizes(const unison_kv_pool* p, const unison_kv_seqs* s, KvArgs& a) {
+  if (!p || !s) return UNISON_E_INVALID;
+  if (p->dtype > UNISON_KV_FP16) return UNISON_E_INVALID;
+  if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return UNISON_E_INVALID;
+  if (p->n_kv < 1 || p->n_kv > kMaxKvHeads) return UNISON_E_INVALID;
+  if (p->page < 16 || p->page > 256 || (p->page & (p->page - 1u))) return UNISON_E_INVALID;
+  if (p->n_pages < 1 || p->n_pages > 0x7FFFFFFFu) return UNISON_E_INVALID;
+  if (s->n_seq > kMaxSeqs) return UNISON_E_CAPACITY;
+  if (s->max_pages < 1 || s->n_tok > 0x7FFFFFFFu) return UNISON_E_INVALID;
+  const uint64_t entries = (uint64_t)s->max_pages * p->page;
+  if (entries > kMaxEntries) return UNISON_E_CAPACITY;
+  if (s->max_len > entries) return UNISON_E_INVALID;
+  if (s->n_tok && s->max_new < 1) return UNISON_E_INVALID;
+  a = KvArgs{};
+  a.dtype = p->dtype;
+  a.dim = p->head_dim;
+  a.n_kv = p->n_kv;
+  a.page = p->page;
+  a.page_bits = (uint32_t)__builtin_ctz(p->page);
+  a.n_pages = p->n_pages;
+  a.k = p->k;
+  a.v = p->v;
+  a.weight = p->weight;
+  a.pos = p->pos;
+  a.box = p->box;
+  a.box_scale = p->box_scale;
+  a.n_seq = s->n_seq;
+  a.max_pages = s->max_pages;
+  a.n_tok = s->n_tok;
+  a.max_new = s->max_new < s->n_tok ? s->max_new : s->n_tok;
+  a.max_len = s->max_len ? s->max_len : (uint32_t)entries;
+  a.pages = s->pages;
+  a.len = s->len;
+  a.tok = s->tok;
+  return UNISON_OK;
+}
+
+int pointers(const KvArgs& a, bool tokens) {
+  if (!on(a.k, 16) || !on(a.v, 16) || !on(a.pages, 4) || !on(a.len, 4)) return UNISON_E_INVALID;
+  if ((a.weight && !on(a.weight, 16)) || (a.pos && !on(a.pos, 16))) return UNISON_E_INVALID;
+  if (!a.box != !a.box_scale || (a.box && (!on(a.box, 16) || !on(a.box_scale, 16)))) return UNISON_E_INVALID;
+  return tokens && !on(a.tok, 4) ? UNISON_E_INVALID : UNISON_OK;
+}
+
+bool rows(const unison_kv_rows* r, KvRows& out) {
+  if (!r || !on(r->p, 16) || r->tok_stride % 8 || r->head_stride % 8) return false;
+  if (r->tok_stride >> 40 || r->head_stride >> 40) return false;
+  out = KvRows{r->p, r->tok_stride, r->head_stride};
+  return true;
+}
+
+int heads(KvArgs& a, uint32_t n_q) {
+  if (n_q < 1 || n_q % a.n_kv || n_q / a.n_kv > kMaxGroup) return UNISON_E_INVALID;
+  a.n_q = n_q;
+  a.group = n_q / a.n_kv;
+  // rows of the token arrays and blocks of a launch are counted in 31 bits
+  return (uint64_t)a.n_tok * n_q > 0x7FFFFFFFull ? UNISON_E_CAPACITY : UNISON_OK;
+}
+
+int done(hipError_t rc) { return rc == hipSuccess ? UNISON_OK : UNISON_E_HIP; }
+
+int attend(void* hip_stream, void* ws, size_t ws_bytes, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
+           uint32_t n_q, const unison_kv_rows* q, float scale, int weights, float decay, uint32_t n_sel,
+           uint32_t first, uint32_t last, void* out, float* lse, int32_t* sel) {
+  KvArgs a;
+  KvRows r;
+  int rc = sizes(pool, seqs, a);
+  if (rc == UNISON_OK) rc = heads(a, n_q);
+  if (rc != UNISON_OK) return rc;
+  if (!std::isfinite(scale)) return UNISON_E_INVALID;
+  if (weights && (!a.weight || !(decay >= 0.0f && decay <= 1.0f))) return UNISON_E_INVALID;
+  if (a.n_seq == 0 || a.n_tok == 0) return UNISON_OK;
+  rc = pointers(a, true);
+  if (rc != UNISON_OK) return rc;
+  if (!rows(q, r) || !on(out, 16) || (lse && !on(lse, 4))) return UNISON_E_INVALID;
+  const size_t need = kv_attend_bytes(a, weights != 0, n_sel);
+  if (need && (ws_bytes < need || !on(ws, 256))) return UNISON_E_INVALID;
+  return done(launch_kv_attend(a, r, scale, weights != 0, decay, n_sel, first, last, out, lse, sel, ws,
+                               reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+int unison_kv_append(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
+                     const unison_kv_rows* k, const unison_kv_rows* v, const int32_t* tok_pos) {
+  KvArgs a;
+  KvRows rk, rv;
+  int rc = sizes(pool, seqs, a);
+  if (rc != UNISON_OK) return rc;
+  if (a.n_seq == 0 || a.n_tok == 0) return UNISON_OK;
+  rc = pointers(a, true);
+  if (rc != UNISON_OK) return rc;
+  if (!rows(k, rk) || !rows(v, rv) || !a.pos != !tok_pos || (tok_pos && !on(tok_pos, 4))) return UNISON_E_INVALID;
+  return done(launch_kv_append(a, rk, rv, tok_pos, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int unison_kv_attend_size(const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t n_q, int weights,
+                          uint32_t n_sel, size_t* bytes) {
+  KvArgs a;
+  int rc = sizes(pool, seqs, a);
+  if (rc == UNISON_OK) rc = heads(a, n_q);
+  if (rc != UNISON_OK) return rc;
+  if (!bytes) return UNISON_E_INVALID;
+  if (n_sel && a.max_pages > kMaxSelPages) return UNISON_E_CAPACITY;
+  *bytes = a.n_seq && a.n_tok ? kv_attend_bytes(a, weights != 0, n_sel) : 0;
+  return UNISON_OK;
+}
+
+int unison_kv_attend(void* hip_stream, void* workspace, size_t workspace_bytes, const unison_kv_pool* pool,
+                     const unison_kv_seqs* seqs, uint32_t n_q, const unison_kv_rows* q, float scale, int weights,
+                     float decay, void* out, float* lse) {
+  return attend(hip_stream, workspace, workspace_bytes, pool, seqs, n_q, q, scale, weights, decay, 0, 0, 0, out, lse,
+                nullptr);
+}
+
+int unison_kv_attend_blocks(void* hip_stream, void* workspace, size_t workspace_bytes, const unison_kv_pool* pool,
+                            const unison_kv_seqs* seqs, uint32_t n_q, const unison_kv_rows* q, float scale,
+                            uint32_t n_sel, uint32_t first, uint32_t last, void* out, float* lse, int32_t* sel) {
+  if (!pool || !seqs || n_sel < 1 || n_sel > kMaxSel || last < 1 || (uint64_t)first + last > n_sel)
+    return UNISON_E_INVALID;
+  if (seqs->max_pages > kMaxSelPages) return UNISON_E_CAPACITY;
+  if (seqs->n_seq && seqs->n_tok && (!pool->box || !on(sel, 4))) return UNISON_E_INVALID;
+  return attend(hip_stream, workspace, workspace_bytes, pool, seqs, n_q, q, scale, 0, 0.0f, n_sel, first, last, out,
+                lse, sel);
+}
+
+int unison_kv_victims(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t budget,
+                      uint32_t first, uint32_t recent, uint32_t max_evict, int32_t* victims, int32_t* src,
+                      int32_t* new_len) {
+  KvArgs a;
+  int rc = sizes(pool, seqs, a);
+  if (rc != UNISON_OK) return rc;
+  if (budget < 1 || (uint64_t)first + recent > budget || max_evict < 1 || max_evict > kMaxEntries)
+    return UNISON_E_INVALID;
+  if (a.n_seq == 0) return UNISON_OK;
+  rc = pointers(a, false);
+  if (rc != UNISON_OK) return rc;
+  if (!a.weight || !a.pos || !on(victims, 4) || !on(src, 4) || !on(new_len, 4)) return UNISON_E_INVALID;
+  return done(launch_kv_victims(a, budget, first, recent, max_evict, victims, src, new_len,
+                                reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+int unison_kv_compact(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t max_evict,
+                      const int32_t* victims, const int32_t* src, const int32_t* new_len) {
+  KvArgs a;
+  int rc = sizes(pool, seqs, a);
+  if (rc != UNISON_OK) return rc;
+  if (max_evict < 1 || max_evict > kMaxEntries) return UNISON_E_INVALID;
+  if (a.n_seq == 0) return UNISON_OK;
+  rc = pointers(a, false);
+  if (rc != UNISON_OK) return rc;
+  if (!on(victims, 4) || !on(src, 4) || !on(new_len, 4)) return UNISON_E_INVALID;
+  return done(launch_kv_compact(a, max_evict, victims, src, new_len, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,277 @@
+"""Python binding of the paged-KV operators (argument marshalling only).
+
+A Pool is the pages of the sessions that the residency policy kept, a Seqs the
+batch of sequences over it; append, attend, attend_blocks, victims and compact
+are the calls of include/unison.h with the same meaning.  Every call runs on
+the current stream of the tensors' device and allocates its outputs and its
+workspace with torch, so calls on several streams or in several captured
+graphs do not share memory.  The tensors behind a Pool and a Seqs stay where
+they are: lengths and page tables are updated in place.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from .unison import E_INVALID, UnisonError, _check, lib
+
+BF16, FP16 = 0, 1
+
+
+class PoolArgs(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("head_dim", C.c_uint32), ("n_kv", C.c_uint32), ("page", C.c_uint32),
+                ("n_pages", C.c_uint32), ("pad0", C.c_uint32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("weight", C.c_void_p), ("pos", C.c_void_p), ("box", C.c_void_p), ("box_scale", C.c_void_p)]
+
+
+class SeqsArgs(C.Structure):
+    _fields_ = [("n_seq", C.c_uint32), ("max_pages", C.c_uint32), ("n_tok", C.c_uint32), ("max_new", C.c_uint32),
+                ("max_len", C.c_uint32), ("pad0", C.c_uint32), ("pages", C.c_void_p), ("len", C.c_void_p),
+                ("tok", C.c_void_p)]
+
+
+class RowsArgs(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("tok_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+_lib = None
+
+
+def _kv():
+    global _lib
+    if _lib is None:
+        L = lib()
+        vp, u32, f32, size = C.c_void_p, C.c_uint32, C.c_float, C.c_size_t
+        pool, seqs, rows = C.POINTER(PoolArgs), C.POINTER(SeqsArgs), C.POINTER(RowsArgs)
+        sig = {
+            "unison_kv_append": [vp, pool, seqs, rows, rows, vp],
+            "unison_kv_attend_size": [pool, seqs, u32, C.c_int, u32, C.POINTER(size)],
+            "unison_kv_attend": [vp, vp, size, pool, seqs, u32, rows, f32, C.c_int, f32, vp, vp],
+            "unison_kv_attend_blocks": [vp, vp, size, pool, seqs, u32, rows, f32, u32, u32, u32, vp, vp, vp],
+            "unison_kv_victims": [vp, pool, seqs, u32, u32, u32, u32, vp, vp, vp],
+            "unison_kv_compact": [vp, pool, seqs, u32, vp, vp, vp],
+        }
+        for name, args in sig.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = C.c_int
+        _lib = L
+    return _lib
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _refuse(why):
+    raise UnisonError(E_INVALID, why)
+
+
+def _need(t, name, dtype, shape, device):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        _refuse("%s: contiguous %s %s on %s wanted, got %s %s on %s" % (
+            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+
+
+class Pool:
+    """Pages of a KV pool: k [n_pages, n_kv, page, head_dim], v [n_pages, n_kv, head_dim, page] in
+    bfloat16 or float16; weight (float32) and pos (int32) [n_pages, n_kv, page]; box (int8)
+    [n_pages, n_kv, 2, head_dim] with box_scale (float32) [n_pages, n_kv]."""
+
+    def __init__(self, k, v, weight=None, pos=None, box=None, box_scale=None):
+        torch = _torch()
+        if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16):
+            _refuse("k: bfloat16 or float16 [n_pages, n_kv, page, head_dim] wanted")
+        n_pages, n_kv, page, dim = k.shape
+        _need(k, "k", k.dtype, k.shape, k.device)
+        _need(v, "v", k.dtype, (n_pages, n_kv, dim, page), k.device)
+        words = (n_pages, n_kv, page)
+        if weight is not None:
+            _need(weight, "weight", torch.float32, words, k.device)
+        if pos is not None:
+            _need(pos, "pos", torch.int32, words, k.device)
+        if (box is None) != (box_scale is None):
+            _refuse("box and box_scale come together")
+        if box is not None:
+            _need(box, "box", torch.int8, (n_pages, n_kv, 2, dim), k.device)
+            _need(box_scale, "box_scale", torch.float32, (n_pages, n_kv), k.device)
+        self.k, self.v, self.weight, self.pos, self.box, self.box_scale = k, v, weight, pos, box, box_scale
+        self.n_kv, self.page, self.head_dim, self.dtype, self.device = n_kv, page, dim, k.dtype, k.device
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self._args = PoolArgs(BF16 if k.dtype == torch.bfloat16 else FP16, dim, n_kv, page, n_pages, 0, ptr(k), ptr(v),
+                              ptr(weight), ptr(pos), ptr(box), ptr(box_scale))
+        self._ref = C.byref(self._args)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv, page, head_dim, dtype=None, device="cuda", weight=True, pos=True, box=False):
+        """A pool of zeroed pages."""
+        torch = _torch()
+        dtype = dtype or torch.bfloat16
+        z = lambda *shape, dt: torch.zeros(shape, dtype=dt, device=device)
+        return cls(z(n_pages, n_kv, page, head_dim, dt=dtype), z(n_pages, n_kv, head_dim, page, dt=dtype),
+                   z(n_pages, n_kv, page, dt=torch.float32) if weight else None,
+                   z(n_pages, n_kv, page, dt=torch.int32) if pos else None,
+                   z(n_pages, n_kv, 2, head_dim, dt=torch.int8) if box else None,
+                   z(n_pages, n_kv, dt=torch.float32) if box else None)
+
+
+class Seqs:
+    """A batch of sequences: pages int32 [n_seq, max_pages] (-1: no page), length int32 [n_seq] with
+    the new tokens counted, tok int32 [n_seq + 1] the ranges of the new tokens' rows.  n_tok, max_new
+    and max_len bound what the device arrays hold (max_len 0: the page table's capacity)."""
+
+    def __init__(self, pages, length, tok=None, n_tok=0, max_new=0, max_len=0):
+        torch = _torch()
+        if pages.dim() != 2:
+            _refuse("pages: int32 [n_seq, max_pages] wanted")
+        n_seq, max_pages = pages.shape
+        _need(pages, "pages", torch.int32, pages.shape, pages.device)
+        _need(length, "length", torch.int32, (n_seq,), pages.device)
+        if tok is not None:
+            _need(tok, "tok", torch.int32, (n_seq + 1,), pages.device)
+        elif n_tok:
+            _refuse("tok is needed where there are new tokens")
+        for name, x in (("n_tok", n_tok), ("max_new", max_new), ("max_len", max_len)):
+            if not 0 <= int(x) < 1 << 31:
+                _refuse("%s out of range" % name)
+        self.pages, self.length, self.tok, self.n_tok, self.n_seq = pages, length, tok, int(n_tok), n_seq
+        self.device = pages.device
+        self._args = SeqsArgs(n_seq, max_pages, int(n_tok), int(max_new), int(max_len), 0, pages.data_ptr(),
+                              length.data_ptr(), None if tok is None else tok.data_ptr())
+        self._ref = C.byref(self._args)
+        self._sizes = {}  # workspace bytes by the pool's sizes and the call's: no content is kept
+
+
+class _On:
+    """The device of a call made current, and its stream."""
+
+    __slots__ = ("device", "before")
+
+    def __init__(self, pool, seqs):
+        if seqs.device != pool.device:
+            _refuse("the sequences are on %s, the pool on %s" % (seqs.device, pool.device))
+        self.device = pool.device
+
+    def __enter__(self):
+        torch = _torch()
+        if self.device.type != "cuda":
+            _refuse("the operators run on the GPU, the pool is on %s" % self.device)
+        self.before = torch.cuda.current_device()
+        if self.before != self.device.index:
+            torch.cuda.set_device(self.device)
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.before != self.device.index:
+            _torch().cuda.set_device(self.before)
+
+
+def _rows(t, name, pool, n_tok, heads):
+    if t.dim() != 3 or t.dtype != pool.dtype or t.device != pool.device or t.shape[0] != n_tok or \
+            t.shape[2] != pool.head_dim or (heads is not None and t.shape[1] != heads):
+        _refuse("%s: %s [%d, heads, %d] on %s wanted, got %s %s on %s" % (
+            name, pool.dtype, n_tok, pool.head_dim, pool.device, t.dtype, tuple(t.shape), t.device))
+    s = t.stride()
+    if s[2] != 1 or s[0] < 0 or s[1] < 0:
+        _refuse("%s: the head dimension has to be contiguous" % name)
+    # the stride of a single row or head is never walked
+    return RowsArgs(t.data_ptr(), s[0] if t.shape[0] > 1 else 0, s[1] if t.shape[1] > 1 else 0)
+
+
+def _int32(t, name, shape, device):
+    _need(t, name, _torch().int32, shape, device)
+    return t.data_ptr()
+
+
+def append(pool, seqs, k, v, positions=None):
+    """Writes the new tokens' rows k, v [n_tok, n_kv, head_dim] (any strides with a contiguous last
+    dimension that are multiples of 8) into their entries; positions int32 [n_tok] where the pool
+    keeps them."""
+    with _On(pool, seqs) as stream:
+        rk, rv = _rows(k, "k", pool, seqs.n_tok, pool.n_kv), _rows(v, "v", pool, seqs.n_tok, pool.n_kv)
+        pos = None if positions is None else _int32(positions, "positions", (seqs.n_tok,), pool.device)
+        _check(_kv().unison_kv_append(stream, pool._ref, seqs._ref, C.byref(rk), C.byref(rv), pos))
+
+
+def _workspace(pool, seqs, n_q, weights, n_sel):
+    key = (pool._args.dtype, pool.head_dim, pool.n_kv, pool.page, n_q, weights, n_sel)
+    n = seqs._sizes.get(key)
+    if n is None:
+        out = C.c_size_t()
+        _check(_kv().unison_kv_attend_size(pool._ref, seqs._ref, n_q, weights, n_sel, C.byref(out)))
+        n = seqs._sizes[key] = out.value
+    return n, _torch().empty(n, dtype=_torch().uint8, device=pool.device) if n else None
+
+
+def _scale(scale, pool):
+    return pool.head_dim ** -0.5 if scale is None else scale
+
+
+def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
+    """Attention of the new tokens q [n_tok, n_q, head_dim] over their sequences; scale: default
+    1 / sqrt(head_dim).  decay: pool.weight becomes decay * weight + the tokens' attention weights
+    (None: it stays).  Returns out, or (out, lse [n_tok, n_q]) with lse = True."""
+    torch = _torch()
+    with _On(pool, seqs) as stream:
+        r = _rows(q, "q", pool, seqs.n_tok, None)
+        n_q = q.shape[1]
+        if out is None:
+            out = torch.empty((seqs.n_tok, n_q, pool.head_dim), dtype=pool.dtype, device=pool.device)
+        else:
+            _need(out, "out", pool.dtype, (seqs.n_tok, n_q, pool.head_dim), pool.device)
+        e = torch.empty((seqs.n_tok, n_q), dtype=torch.float32, device=pool.device) if lse else None
+        n, ws = _workspace(pool, seqs, n_q, int(decay is not None), 0)
+        _check(_kv().unison_kv_attend(stream, None if ws is None else ws.data_ptr(), n, pool._ref, seqs._ref, n_q,
+                                      C.byref(r), _scale(scale, pool), int(decay is not None), decay or 0.0,
+                                      out.data_ptr(), None if e is None else e.data_ptr()))
+    return (out, e) if lse else out
+
+
+def attend_blocks(pool, seqs, q, n_sel, first=0, last=1, scale=None, lse=False):
+    """The same over at most n_sel pages a token and kv head: the first and the last of those it sees
+    and the ones of highest box score.  Returns (out, sel int32 [n_tok, n_kv, n_sel]) and lse."""
+    torch = _torch()
+    with _On(pool, seqs) as stream:
+        r = _rows(q, "q", pool, seqs.n_tok, None)
+        n_q = q.shape[1]
+        for name, x in (("n_sel", n_sel), ("first", first), ("last", last)):
+            if not 0 <= x < 1 << 31:
+                _refuse("%s out of range" % name)
+        if not 1 <= n_sel <= 4096:
+            _refuse("n_sel out of range")
+        out = torch.empty((seqs.n_tok, n_q, pool.head_dim), dtype=pool.dtype, device=pool.device)
+        sel = torch.empty((seqs.n_tok, pool.n_kv, n_sel), dtype=torch.int32, device=pool.device)
+        e = torch.empty((seqs.n_tok, n_q), dtype=torch.float32, device=pool.device) if lse else None
+        n, ws = _workspace(pool, seqs, n_q, 0, n_sel)
+        _check(_kv().unison_kv_attend_blocks(stream, None if ws is None else ws.data_ptr(), n, pool._ref, seqs._ref,
+                                             n_q, C.byref(r), _scale(scale, pool), n_sel, first, last, out.data_ptr(),
+                                             None if e is None else e.data_ptr(), sel.data_ptr()))
+    return (out, sel, e) if lse else (out, sel)
+
+
+def victims(pool, seqs, budget, first=0, recent=0, max_evict=1):
+    """The entries that leave sequences of more than `budget`, by least weight: (victims, src, new_len),
+    int32 [n_seq, n_kv, max_evict] twice and [n_seq]."""
+    torch = _torch()
+    with _On(pool, seqs) as stream:
+        for name, x in (("budget", budget), ("first", first), ("recent", recent), ("max_evict", max_evict)):
+            if not 0 <= x < 1 << 31:
+                _refuse("%s out of range" % name)
+        shape = (seqs.n_seq, pool.n_kv, max_evict)
+        gone = torch.empty(shape, dtype=torch.int32, device=pool.device)
+        src = torch.empty(shape, dtype=torch.int32, device=pool.device)
+        new_len = torch.empty(seqs.n_seq, dtype=torch.int32, device=pool.device)
+        _check(_kv().unison_kv_victims(stream, pool._ref, seqs._ref, budget, first, recent, max_evict,
+                                       gone.data_ptr(), src.data_ptr(), new_len.data_ptr()))
+    return gone, src, new_len
+
+
+def compact(pool, seqs, victims, src, new_len):
+    """Carries victims()'s lists out; afterwards the caller sets the lengths to new_len."""
+    with _On(pool, seqs) as stream:
+        if victims.dim() != 3:
+            _refuse("victims: int32 [n_seq, n_kv, max_evict] wanted")
+        shape = (seqs.n_seq, pool.n_kv, victims.shape[2])
+        v, s = _int32(victims, "victims", shape, pool.device), _int32(src, "src", shape, pool.device)
+        n = _int32(new_len, "new_len", (seqs.n_seq,), pool.device)
+        _check(_kv().unison_kv_compact(stream, pool._ref, seqs._ref, shape[2], v, s, n))

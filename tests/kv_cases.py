@@ -1,0 +1,253 @@
+"""A plain implementation of the paged-KV operators in 64 bits (numpy), and the pools the tests run
+them on.  Slots that no sequence owns, and entries at and past a length, hold NaN."""
+import numpy as np
+
+HALF = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}   # half a step of a rounding, relative
+
+
+def to_type(x, dtype):
+    """Values of `x` rounded to the type, as float64."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float16
+    return torch.from_numpy(np.asarray(x, np.float64)).to(t).double().numpy()
+
+
+class Case:
+    """Pages of a few sequences on the host: k [pages][n_kv][page][dim], v transposed."""
+
+    def __init__(self, dtype="bf16", dim=64, page=16, n_kv=2, group=2, lens=(5,), new=(1,), seed=0, spare=2,
+                 max_pages=None, missing=(), sharp=1.5, tail=0, ties=False):
+        r = np.random.Generator(np.random.PCG64(seed))
+        self.dtype, self.dim, self.page, self.n_kv, self.group = dtype, dim, page, n_kv, group
+        self.lens, self.new = list(lens), list(new)
+        need = [-(-n // page) for n in lens]
+        self.max_pages = max_pages or max(1, max(need, default=1))
+        self.n_pages = sum(need) + spare
+        order = r.permutation(self.n_pages)
+        self.pages = np.full((len(lens), self.max_pages), -1, np.int32)
+        at = 0
+        for i, n in enumerate(need):
+            self.pages[i, :n] = order[at:at + n]
+            at += n
+        shape = (self.n_pages, n_kv, page, dim)
+        k = r.standard_normal(shape) + 0.5 * r.standard_normal((self.n_pages, n_kv, 1, dim))
+        v = r.standard_normal((self.n_pages, n_kv, dim, page))
+        weight = r.random((self.n_pages, n_kv, page)) if not ties else r.integers(0, 4, (self.n_pages, n_kv, page))
+        live = np.zeros((self.n_pages, page), bool)
+        self.pos = np.zeros((self.n_pages, n_kv, page), np.int32)
+        for i, n in enumerate(lens):
+            for h in range(n_kv):
+                p = r.permutation(2 * n)[:n] if n else []
+                for e in range(n):
+                    self.pos[self.pages[i, e // page], h, e % page] = p[e]
+            for e in range(n):
+                live[self.pages[i, e // page], e % page] = True
+        k = np.where(live[:, None, :, None], to_type(k, dtype), np.nan)
+        v = np.where(live[:, None, None, :], to_type(v, dtype), np.nan)
+        self.k, self.v = k, v
+        self.weight = np.where(live[:, None, :], weight.astype(np.float32), np.float32(np.nan))
+        for i, o in missing:
+            self.pages[i, o] = -1 if (i + o) % 2 else self.n_pages + 3
+        self.tok = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+        self.n_tok = int(self.tok[-1]) + tail
+        self.q = to_type(sharp * r.standard_normal((self.n_tok, n_kv * group, dim)), dtype)
+        self.new_k = to_type(r.standard_normal((self.n_tok, n_kv, dim)), dtype)
+        self.new_v = to_type(r.standard_normal((self.n_tok, n_kv, dim)), dtype)
+        self.box = np.zeros((self.n_pages, n_kv, 2, dim), np.int8)
+        self.box_scale = np.zeros((self.n_pages, n_kv), np.float32)
+        for i, n in enumerate(lens):
+            for o in range(-(-n // page)):
+                self.rebox(i, o, n)
+
+    def there(self, i, o):
+        return 0 <= self.pages[i, o] < self.n_pages
+
+    def rebox(self, i, o, n):
+        """The box of a sequence's page over its entries below n."""
+        if not self.there(i, o):
+            return
+        p = self.pages[i, o]
+        for h in range(self.n_kv):
+            rows = self.k[p, h, :min(self.page, n - o * self.page)]
+            top = np.abs(rows).max()
+            if top < 2.0 ** -120:
+                self.box[p, h], self.box_scale[p, h] = 0, 0.0
+                continue
+            step = 2.0 ** (np.frexp(top)[1] - 7)
+            self.box[p, h, 0] = np.clip(np.floor(rows.min(0) / step), -127, 127)
+            self.box[p, h, 1] = np.clip(np.ceil(rows.max(0) / step), -127, 127)
+            self.box_scale[p, h] = step
+
+    def rows(self, i):
+        """(token row, its limit) of a sequence's new tokens."""
+        return [(self.tok[i] + j, self.lens[i] - self.new[i] + j + 1) for j in range(self.new[i])]
+
+    def entries(self, i, h, n):
+        """Entry numbers below n that are there, their keys and values."""
+        e = np.array([x for x in range(max(n, 0)) if self.there(i, x // self.page)], np.int64)
+        p, s = self.pages[i, e // self.page], e % self.page
+        return e, self.k[p, h, s], self.v[p, h, :, s]
+
+    def attend(self, scale, chosen=None):
+        """out, lse, the tokens' weights per entry [n_seq][n_kv][len], and for each the derived bounds of
+        a computation that rounds p and the result to the type and sums in 32 bits."""
+        n_q = self.n_kv * self.group
+        out = np.zeros((self.n_tok, n_q, self.dim))
+        lse = np.full((self.n_tok, n_q), -np.inf)
+        tol_out, tol_lse = np.zeros_like(out), np.zeros_like(lse)
+        got = [np.zeros((self.n_kv, n)) for n in self.lens]
+        tol_got = [np.zeros((self.n_kv, n)) for n in self.lens]
+        half, step = HALF[self.dtype], 2.0 ** -24
+        for i in range(len(self.lens)):
+            for h in range(self.n_kv):
+                all_e, all_k, all_v = self.entries(i, h, self.lens[i])
+                for t, limit in self.rows(i):
+                    use = all_e < limit
+                    if chosen is not None:
+                        use &= np.isin(all_e // self.page, chosen[t, h])
+                    e, k, v = all_e[use], all_k[use], all_v[use]
+                    if not len(e):
+                        continue
+                    for g in range(self.group):
+                        hq = h * self.group + g
+                        s = scale * (k @ self.q[t, hq])
+                        x = np.exp(s - s.max())
+                        l = x.sum()
+                        p = x / l
+                        out[t, hq], lse[t, hq] = p @ v, s.max() + np.log(l)
+                        got[i][h, e] += p
+                        # a score: dim products summed in 32 bits, then a few roundings of its own size
+                        # and of the maximum's and lse's
+                        ds = (self.dim + 2) * step * abs(scale) * (np.abs(k) @ np.abs(self.q[t, hq])).max() \
+                            + 8 * step * (np.abs(s).max() + abs(lse[t, hq]))
+                        # exp and its sum: a few steps, and at most one for each of the terms added one by one
+                        dp = 2 * ds + (16 + len(e)) * step
+                        a = p @ np.abs(v)
+                        # a p below fp16's normal range keeps an absolute error, relative to the largest term
+                        low = 2.0 ** -25 * np.abs(v).sum(0) if self.dtype == "fp16" else 0.0
+                        tol_out[t, hq] = half * np.abs(out[t, hq]) + (half * 1.01 + dp) * a + low + 2.0 ** -24
+                        tol_lse[t, hq] = ds + dp + 8 * step
+                        tol_got[i][h, e] += p * dp + 2.0 ** -126
+        return out, lse, got, tol_out, tol_lse, tol_got
+
+    def choose(self, n_sel, first, last):
+        sel = np.full((self.n_tok, self.n_kv, n_sel), -1, np.int32)
+        for i in range(len(self.lens)):
+            for h in range(self.n_kv):
+                for t, limit in self.rows(i):
+                    q = self.q[t, h * self.group:(h + 1) * self.group]
+                    top = np.abs(q).max()
+                    qi = np.zeros_like(q)
+                    if top >= 2.0 ** -120:
+                        qi = np.clip(np.rint(q * 2.0 ** (7 - np.frexp(top)[1])), -127, 127)
+                    count = -(-max(limit, 0) // self.page)
+                    keys = []
+                    for o in range(count):
+                        if not self.there(i, o):
+                            continue
+                        b = self.box[self.pages[i, o], h].astype(np.float64)
+                        score = np.float32(np.maximum(qi * b[0], qi * b[1]).sum()) * \
+                            self.box_scale[self.pages[i, o], h]
+                        must = o < first or o >= count - last
+                        keys.append((0 if must else 1, 0.0 if must else -float(score), o))
+                    use = sorted(o for _, _, o in sorted(keys)[:n_sel])
+                    sel[t, h, :len(use)] = use
+        return sel
+
+    def victims(self, budget, first, recent, max_evict):
+        n_seq = len(self.lens)
+        gone = np.full((n_seq, self.n_kv, max_evict), -1, np.int32)
+        src = np.full((n_seq, self.n_kv, max_evict), -1, np.int32)
+        new_len = np.zeros(n_seq, np.int32)
+        for i, length in enumerate(self.lens):
+            n = min(max(0, length - budget), max_evict)
+            new_len[i] = length - n
+            for h in range(self.n_kv):
+                w, pos, there = np.zeros(length), np.zeros(length, np.int64), np.zeros(length, bool)
+                for e in range(length):
+                    if self.there(i, e // self.page):
+                        p, there[e] = self.pages[i, e // self.page], True
+                        w[e], pos[e] = self.weight[p, h, e % self.page], self.pos[p, h, e % self.page]
+                w = np.where(np.isnan(w), 0.0, w)
+                newest = pos[there].max() if there.any() else 0
+                keep = ~there | (pos < first) | (pos > newest - recent)
+                out = sorted(range(length), key=lambda e: (keep[e], 0.0 if keep[e] else w[e], e))[:n]
+                out = sorted(out)
+                gone[i, h, :n] = out
+                fill = [e for e in range(length - n, length) if e not in set(out)]
+                src[i, h, :len(fill)] = fill
+        return gone, src, new_len
+
+    def compact(self, gone, src, new_len):
+        """The pool after the moves, as a copy of this case."""
+        import copy
+        c = copy.deepcopy(self)
+        for i in range(len(self.lens)):
+            touched = set()
+            for h in range(self.n_kv):
+                for to, fr in zip(gone[i, h], src[i, h]):
+                    if fr < 0:
+                        continue
+                    if not (self.there(i, to // self.page) and self.there(i, fr // self.page)):
+                        continue
+                    a, b = self.pages[i, to // self.page], self.pages[i, fr // self.page]
+                    x, y = to % self.page, fr % self.page
+                    c.k[a, h, x], c.v[a, h, :, x] = self.k[b, h, y], self.v[b, h, :, y]
+                    c.weight[a, h, x], c.pos[a, h, x] = self.weight[b, h, y], self.pos[b, h, y]
+                    touched.add(to // self.page)
+            if new_len[i] < self.lens[i]:
+                touched |= {o for o in range(-(-int(new_len[i]) // self.page)) if (o + 1) * self.page > new_len[i]}
+            for o in touched:
+                c.rebox(i, o, int(new_len[i]))
+            c.lens[i] = int(new_len[i])
+        return c
+
+    def append(self, positions):
+        import copy
+        c = copy.deepcopy(self)
+        for i, length in enumerate(self.lens):
+            first, touched = length - self.new[i], set()
+            for j in range(self.new[i]):
+                e, t = first + j, self.tok[i] + j
+                if e < 0 or not self.there(i, e // self.page):
+                    continue
+                p, s = self.pages[i, e // self.page], e % self.page
+                c.k[p, :, s], c.v[p, :, :, s] = self.new_k[t], self.new_v[t]
+                c.weight[p, :, s], c.pos[p, :, s] = 0.0, positions[t]
+                touched.add(e // self.page)
+            for o in touched:
+                c.rebox(i, o, length)
+        return c
+
+
+# ------------------------------------------------------------------ on the GPU
+
+def device(c, parts=("weight", "pos", "box"), tok=True, max_new=None, max_len=0):
+    """The case's pool and batch as the framework's objects."""
+    import torch
+    from paper_2609_09643_amd import kv
+    dt = torch.bfloat16 if c.dtype == "bf16" else torch.float16
+    g = lambda a, t: torch.from_numpy(np.ascontiguousarray(a)).to(t).cuda()
+    pool = kv.Pool(g(c.k, dt), g(c.v, dt), g(c.weight, torch.float32) if "weight" in parts else None,
+                   g(c.pos, torch.int32) if "pos" in parts else None, g(c.box, torch.int8) if "box" in parts else None,
+                   g(c.box_scale, torch.float32) if "box" in parts else None)
+    seqs = kv.Seqs(g(c.pages, torch.int32), g(np.array(c.lens), torch.int32), g(c.tok, torch.int32), n_tok=c.n_tok,
+                   max_new=max_new or max([1] + c.new), max_len=max_len)
+    return pool, seqs
+
+
+def rows(x, dtype):
+    import torch
+    return torch.from_numpy(x).to(torch.bfloat16 if dtype == "bf16" else torch.float16).cuda()
+
+
+def near(got, want, tol, label):
+    """Every value within its own bound; infinities and zeros of empty rows in place."""
+    got = got.double().cpu().numpy()
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isfinite(got), fine), label + ": not finite elsewhere"
+    assert np.array_equal(got[~fine], want[~fine]), label
+    off = np.where(fine, np.abs(np.where(fine, got, 0.0) - np.where(fine, want, 0.0)) - tol, -1.0)
+    worst = np.unravel_index(np.argmax(off), off.shape) if off.size else None
+    assert worst is None or off[worst] <= 0, "%s: at %s %g, wanted %g within %g" % (
+        label, worst, got[worst], want[worst], tol[worst])
