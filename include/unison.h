@@ -460,7 +460,7 @@ typedef struct {
  * share pages in calls that do not write them (attention without weights). */
 typedef struct {
   uint32_t n_seq;       /* 0..65535; 0: the call does nothing */
-  uint32_t max_pages;   /* page ids per sequence; max_pages * page <= 2^30 */
+  uint32_t max_pages;   /* page ids per sequence; max_pages * page <= 2^27 */
   uint32_t n_tok;       /* rows of the token arrays */
   uint32_t max_new;     /* no sequence has more new tokens; >= 1 if n_tok is */
   uint32_t max_len;     /* no sequence is longer; 0: max_pages * page */
@@ -551,7 +551,7 @@ int unison_kv_attend_blocks(void* hip_stream, void* workspace, size_t workspace_
  *                                that moves into its place: the kept entries at
  *                                and past new_len, ascending; else -1
  * Nothing in the pool changes.  Needs the pool's weights and positions;
- * budget >= first + recent, budget >= 1, 1 <= max_evict <= 2^30.  The three
+ * budget >= first + recent, budget >= 1, 1 <= max_evict <= 2^27.  The three
  * arrays are 4-byte aligned.
  * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
 int unison_kv_victims(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,

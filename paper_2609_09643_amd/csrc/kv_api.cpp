@@ -13,6 +13,7 @@ hipError_t launch_kv_victims(const KvArgs& a, uint32_t budget, uint32_t first, u
 hipError_t launch_kv_compact(const KvArgs& a, uint32_t max_evict, const int32_t* victims, const int32_t* src,
                              const int32_t* new_len, hipStream_t st);
 size_t kv_attend_bytes(const KvArgs& a, bool weights, uint32_t n_sel);
+bool kv_attend_fits(const KvArgs& a, uint32_t n_sel);
 hipError_t launch_kv_attend(const KvArgs& a, const KvRows& q, float scale, bool weights, float decay,
                             uint32_t n_sel, uint32_t first, uint32_t last, void* out, float* lse, int32_t* sel,
                             void* ws, hipStream_t st);
@@ -23,7 +24,7 @@ using namespace unison;
 namespace {
 
 constexpr uint32_t kMaxSeqs = 65535, kMaxKvHeads = 1024, kMaxGroup = 128, kMaxSelPages = 32768, kMaxSel = 4096;
-constexpr uint64_t kMaxEntries = 1ull << 30;
+constexpr uint64_t kMaxEntries = 1ull << 27;  // of a sequence: blocks of 16 stay below 2^32 threads a launch
 
 bool on(const void* p, size_t bytes) { return p && reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
@@ -83,7 +84,7 @@ int heads(KvArgs& a, uint32_t n_q) {
   if (n_q < 1 || n_q % a.n_kv || n_q / a.n_kv > kMaxGroup) return UNISON_E_INVALID;
   a.n_q = n_q;
   a.group = n_q / a.n_kv;
-  // rows of the token arrays and blocks of a launch are counted in 31 bits
+  // rows of the token arrays are counted in 31 bits
   return (uint64_t)a.n_tok * n_q > 0x7FFFFFFFull ? UNISON_E_CAPACITY : UNISON_OK;
 }
 
@@ -103,6 +104,7 @@ int attend(void* hip_stream, void* ws, size_t ws_bytes, const unison_kv_pool* po
   rc = pointers(a, true);
   if (rc != UNISON_OK) return rc;
   if (!rows(q, r) || !on(out, 16) || (lse && !on(lse, 4))) return UNISON_E_INVALID;
+  if (!kv_attend_fits(a, n_sel)) return UNISON_E_CAPACITY;
   const size_t need = kv_attend_bytes(a, weights != 0, n_sel);
   if (need && (ws_bytes < need || !on(ws, 256))) return UNISON_E_INVALID;
   return done(launch_kv_attend(a, r, scale, weights != 0, decay, n_sel, first, last, out, lse, sel, ws,
