@@ -744,8 +744,12 @@ size_t kv_attend_bytes(const KvArgs& a, bool weights, uint32_t n_sel) { return p
 bool kv_attend_fits(const KvArgs& a, uint32_t n_sel) {
   const Plan p = plan_of(a, false, n_sel);
   const uint64_t rows = (uint64_t)a.max_new * a.group, most = (1ull << 24) - 1;
-  if (n_sel) return (uint64_t)p.few_split * a.max_new * ((a.group + p.few_rows - 1) / p.few_rows) <= most && rows / (1024 / a.dim) < most;
-  return (uint64_t)a.n_kv * p.many_split <= most && (rows + kManyRows - 1) / kManyRows <= 65535 && rows / (1024 / a.dim) < most;
+  if (rows / (4 * kBlock / a.dim) >= most) return false;
+  if (n_sel) {
+    const uint64_t tiles = (a.group + p.few_rows - 1) / p.few_rows, scored = (a.max_len >> a.page_bits) / 64 + 1;
+    return p.few_split * tiles * a.max_new <= most && scored * a.max_new <= most;
+  }
+  return (uint64_t)a.n_kv * p.many_split <= most && (rows + kManyRows - 1) / kManyRows <= 65535;
 }
 
 hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, uint32_t n_sel, uint32_t first, uint32_t last,

@@ -1,5 +1,7 @@
 // kv_cache.hip -- the operators that write pages or choose among entries: append, victims, compact,
 // and the page choice of sparse attention.
+#include <type_traits>
+
 #include "kv_device.h"
 
 #pragma clang fp contract(off)
@@ -9,46 +11,93 @@ namespace unison {
 namespace {
 
 constexpr uint32_t kBlock = 256;
-constexpr uint32_t kSelBlock = 1024;
 
-// Renews the box of one page of kv head h over its first `live` slots: a thread per dimension (the
-// block has at least `dim`).  All threads of the block call it.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+
 template <typename T>
-__device__ void renew_box(const KvArgs& a, int32_t page, uint32_t h, int32_t live, float* lds) {
-  const uint32_t tid = threadIdx.x;
-  float lo = 0.0f, hi = 0.0f;
-  if (tid < a.dim) {
-    const T* k = (const T*)a.k + kv_base(a, page, h) + tid;
-    lo = __int_as_float(0x7F800000);
-    hi = -lo;
-    for (int32_t i = 0; i < live; ++i) {
-      const float x = to_f32(k[(size_t)i * a.dim]);
-      lo = fminf(lo, x);
-      hi = fmaxf(hi, x);
+__device__ __forceinline__ float bits_f32(uint16_t b);
+template <>
+__device__ __forceinline__ float bits_f32<__hip_bfloat16>(uint16_t b) {
+  return __uint_as_float((uint32_t)b << 16);
+}
+template <>
+__device__ __forceinline__ float bits_f32<__half>(uint16_t b) {
+  return (float)__builtin_bit_cast(_Float16, b);
+}
+
+// ------------------------------------------------------------------ boxes
+
+// The lower and upper sides of a page's keys, gathered 8 dimensions at a time: thread t of the block
+// has the dimensions 8 (t % (D / 8)) of rows t / (D / 8), t / (D / 8) + kBlock / (D / 8), ...
+struct Sides {
+  float lo[8], hi[8];
+  __device__ __forceinline__ void clear() {
+    for (int i = 0; i < 8; ++i) {
+      lo[i] = __builtin_inff();
+      hi[i] = -__builtin_inff();
     }
   }
-  float top = tid < a.dim ? fmaxf(fabsf(lo), fabsf(hi)) : 0.0f;
+  template <typename T>
+  __device__ __forceinline__ void add(u16x8 x) {
+    for (int i = 0; i < 8; ++i) {
+      const float f = bits_f32<T>(x[i]);
+      lo[i] = fminf(lo[i], f);
+      hi[i] = fmaxf(hi[i], f);
+    }
+  }
+};
+
+// Writes a page's box from the threads' sides; `lds` has 16 words a thread.  All threads call it.
+template <int D>
+__device__ void write_box(const KvArgs& a, int32_t page, uint32_t h, const Sides& x, float* lds) {
+  constexpr uint32_t CH = D / 8, RG = kBlock / CH;
+  const uint32_t tid = threadIdx.x, c = tid % CH, g = tid / CH;
+  for (int i = 0; i < 8; ++i) {
+    lds[g * D + 8 * c + i] = x.lo[i];
+    lds[(RG + g) * D + 8 * c + i] = x.hi[i];
+  }
+  __syncthreads();
+  float lo = 0.0f, hi = 0.0f, top = 0.0f;
+  if (tid < D) {
+    lo = lds[tid];
+    hi = lds[RG * D + tid];
+    for (uint32_t i = 1; i < RG; ++i) {
+      lo = fminf(lo, lds[i * D + tid]);
+      hi = fmaxf(hi, lds[(RG + i) * D + tid]);
+    }
+    top = fmaxf(fabsf(lo), fabsf(hi));
+  }
+  __syncthreads();
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if ((tid & 63u) == 0u) lds[tid >> 6] = top;
   __syncthreads();
-  top = 0.0f;
-  for (uint32_t w = 0; w < blockDim.x / 64u; ++w) top = fmaxf(top, lds[w]);
-  __syncthreads();
+  top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
   const KvStep st = kv_step(top);
-  if (tid < a.dim) {
-    int8_t* b = a.box + ((size_t)page * a.n_kv + h) * 2 * a.dim + tid;
+  if (tid < D) {
+    int8_t* b = a.box + ((size_t)page * a.n_kv + h) * 2 * D + tid;
     b[0] = (int8_t)kv_clip(floorf(lo * st.inv));
-    b[a.dim] = (int8_t)kv_clip(ceilf(hi * st.inv));
+    b[D] = (int8_t)kv_clip(ceilf(hi * st.inv));
   }
   if (tid == 0) a.box_scale[(size_t)page * a.n_kv + h] = st.step;
 }
 
-// One block per (page that may get entries, kv head, sequence).
-template <typename T>
+// ------------------------------------------------------------------ append
+
+// One block per (page that may get entries, kv head, sequence).  Keys go over in 16-byte pieces and,
+// where the pool has boxes, through the box's sides on the way, together with the page's older rows.
+// Values change their order: 64 slots of the page are put together in LDS, two slots to a word, and
+// leave in 16-byte runs of slots; up to kDirect new rows (a decode step) go straight to their places.
+constexpr int32_t kDirect = 4;
+
+template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void kv_append_kernel(KvArgs a, KvRows nk, KvRows nv,
                                                            const int32_t* tok_pos) {
-  __shared__ float lds[kBlock / 64];
-  const uint32_t h = blockIdx.y, tid = threadIdx.x;
+  constexpr uint32_t CH = D / 8, RG = kBlock / CH, S = 33;  // an odd stride spreads the words over the banks
+  __shared__ uint32_t lds[D * S > 16 * kBlock ? D * S : 16 * kBlock];
+  const uint32_t h = blockIdx.y, tid = threadIdx.x, c = tid % CH, g = tid / CH;
   const KvSeq q = kv_seq(a, blockIdx.z);
   const int32_t first = q.len - q.n;  // below 0: tokens without an entry
   const int32_t o = ((first < 0 ? 0 : first) >> a.page_bits) + (int32_t)blockIdx.x;
@@ -57,27 +106,270 @@ __global__ __launch_bounds__(kBlock) void kv_append_kernel(KvArgs a, KvRows nk, 
   if (b >= e) return;
   const int32_t page = kv_page(a, q, o);
   if (page < 0) return;
-  T* k = (T*)a.k + kv_base(a, page, h);
-  T* v = (T*)a.v + kv_base(a, page, h);
-  for (uint32_t i = tid; i < (uint32_t)(e - b) * a.dim; i += kBlock) {
-    const uint32_t r = i / a.dim, d = i % a.dim, slot = (uint32_t)(b - lo) + r;
-    const size_t tok = (size_t)(q.t0 + (b - first)) + r;
-    k[(size_t)slot * a.dim + d] = ((const T*)nk.p)[tok * nk.tok + h * nk.head + d];
-    v[(size_t)d * a.page + slot] = ((const T*)nv.p)[tok * nv.tok + h * nv.head + d];
-  }
+  uint16_t* k = (uint16_t*)a.k + kv_base(a, page, h);
+  uint16_t* v = (uint16_t*)a.v + kv_base(a, page, h);
+  const int32_t t0 = q.t0 - first;  // row of entry x: t0 + x
+  const uint16_t* sk = (const uint16_t*)nk.p + h * nk.head + 8 * c;
+  const uint16_t* sv = (const uint16_t*)nv.p + h * nv.head;
   for (int32_t i = b + (int32_t)tid; i < e; i += (int32_t)kBlock) {
     const size_t w = kv_word(a, page, h) + (size_t)(i - lo);
     if (a.weight) a.weight[w] = 0.0f;
-    if (a.pos) a.pos[w] = tok_pos[q.t0 + (i - first)];
+    if (a.pos) a.pos[w] = tok_pos[t0 + i];
   }
-  if (a.box) {
-    __threadfence_block();
-    __syncthreads();
-    renew_box<T>(a, page, h, e - lo, lds);
+  if (e - b <= kDirect) {
+    for (uint32_t i = tid; i < (uint32_t)(e - b) * D; i += kBlock) {
+      const int32_t x = b + (int32_t)(i / D);
+      v[(size_t)(i % D) * a.page + (uint32_t)(x - lo)] = sv[(size_t)(t0 + x) * nv.tok + i % D];
+    }
+  } else {
+    for (int32_t s0 = b & ~63; s0 < e; s0 += 64) {
+      const int32_t base = s0 > lo ? s0 : lo;  // pages of 16 and 32 are narrower than 64 slots
+      const int32_t stop = base + 64 < hi ? base + 64 : hi;
+      for (uint32_t x = g; x < (uint32_t)(stop - base) / 2; x += RG) {
+        const int32_t r = base + 2 * (int32_t)x;
+        u16x8 u = (u16x8)(uint16_t)0, w = (u16x8)(uint16_t)0;
+        if (r >= b && r < e) u = *(const u16x8*)(sv + (size_t)(t0 + r) * nv.tok + 8 * c);
+        if (r + 1 >= b && r + 1 < e) w = *(const u16x8*)(sv + (size_t)(t0 + r + 1) * nv.tok + 8 * c);
+        for (uint32_t i = 0; i < 8; ++i) lds[(8 * c + i) * S + x] = u[i] | ((uint32_t)w[i] << 16);
+      }
+      __syncthreads();
+      const uint32_t runs = (uint32_t)(stop - base) / 8;  // 2, 4 or 8
+      for (uint32_t i = tid; i < D * runs; i += kBlock) {
+        const uint32_t d = i / runs, run = i % runs;
+        const int32_t r = base + 8 * (int32_t)run;
+        const uint32_t* from = lds + d * S + 4 * run;
+        const u32x4 x = {from[0], from[1], from[2], from[3]};
+        uint16_t* to = v + (size_t)d * a.page + (uint32_t)(r - lo);
+        if (r >= b && r + 8 <= e) {
+          *(u32x4*)to = x;
+        } else {
+          for (int32_t y = 0; y < 8; ++y)
+            if (r + y >= b && r + y < e) to[y] = (uint16_t)(x[y >> 1] >> (16 * (y & 1)));
+        }
+      }
+      __syncthreads();
+    }
   }
+  Sides side;
+  side.clear();
+  for (int32_t x = (a.box ? lo : b) + (int32_t)g; x < e; x += (int32_t)RG) {
+    uint16_t* at = k + (size_t)(uint32_t)(x - lo) * D + 8 * c;
+    u16x8 row;
+    if (x >= b) {
+      row = *(const u16x8*)(sk + (size_t)(t0 + x) * nk.tok);
+      *(u16x8*)at = row;
+    } else {
+      row = *(const u16x8*)at;
+    }
+    if (a.box) side.add<T>(row);
+  }
+  if (a.box) write_box<D>(a, page, h, side, (float*)lds);
 }
 
 // ------------------------------------------------------------------ the n smallest keys
+
+// Finds the `need` smallest of up to BLOCK * PER keys that the block holds in registers: element i of
+// a thread is number wave * 64 PER + (i / 4) * 256 + 4 lane + i % 4, so that its memory is read in
+// 16-byte pieces side by side and still follows in the order of numbers.
+template <int BLOCK, int PER>
+struct Pick {
+  uint32_t hist[2048];
+  uint32_t sums[2][BLOCK / 64];
+  uint32_t found[3];
+};
+
+template <int BLOCK, int PER>
+__device__ __forceinline__ uint32_t pick_number(int i) {
+  return (threadIdx.x >> 6) * 64u * PER + (uint32_t)(i / 4) * 256u + 4u * (threadIdx.x & 63u) + (uint32_t)(i % 4);
+}
+
+struct Cut {
+  uint32_t key;   // the largest chosen key
+  uint32_t ties;  // how many entries with that key are chosen: the lowest numbers
+};
+
+// The cut of the `need` smallest keys, 1 <= need <= the keys' count; a key of 0xFFFFFFFF is chosen only when
+// the others do not suffice, and elements at and past `count` hold it.  Digits of 11, 11 and 10 bits from
+// the top: a histogram (whole numbers: any order of additions gives the same), its prefix, and the
+// digit the cut is in.  It ends early once a digit is taken whole.
+template <int BLOCK, int PER>
+__device__ Cut pick_cut(const uint32_t (&key)[PER], uint32_t need, Pick<BLOCK, PER>& s) {
+  constexpr uint32_t BINS = 2048 / BLOCK;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+  for (uint32_t i = 0; i < BINS; ++i) s.hist[tid * BINS + i] = 0;
+  uint32_t prefix = 0, left = need, top = 0;  // bits of the key at and above `top` are known
+  for (int pass = 0; pass < 3; ++pass) {
+    const uint32_t shift = pass == 0 ? 21u : pass == 1 ? 10u : 0u, mask = pass == 2 ? 1023u : 2047u;
+    __syncthreads();
+    for (int i = 0; i < PER; ++i) {
+      const bool in = key[i] != 0xFFFFFFFFu && (pass == 0 || (key[i] >> top) == (prefix >> top));
+      const uint32_t bin = (key[i] >> shift) & mask;
+      const uint64_t who = __builtin_amdgcn_ballot_w64(in);
+      if (who == 0ull) continue;
+      // equal digits in a whole wavefront (weights that were never added to) count once
+      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)bin, (int)__builtin_ctzll(who));
+      if (__builtin_amdgcn_ballot_w64(in && bin == one) == who) {
+        if (lane == 0) atomicAdd(&s.hist[one], (uint32_t)__builtin_popcountll(who));
+      } else if (in) {
+        atomicAdd(&s.hist[bin], 1u);
+      }
+    }
+    __syncthreads();
+    uint32_t n[BINS], sum = 0;
+    for (uint32_t i = 0; i < BINS; ++i) {
+      n[i] = s.hist[tid * BINS + i];
+      s.hist[tid * BINS + i] = 0;
+      sum += n[i];
+    }
+    uint32_t upto = sum;
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t y = __shfl_up(upto, o);
+      if (lane >= (uint32_t)o) upto += y;
+    }
+    if (lane == 63u) s.sums[0][wave] = upto;
+    if (tid == 0) s.found[2] = 0;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (uint32_t w = 0; w < BLOCK / 64; ++w) {
+      before += w < wave ? s.sums[0][w] : 0u;
+      all += s.sums[0][w];
+    }
+    uint32_t at = before + upto - sum;
+    for (uint32_t i = 0; i < BINS; ++i) {
+      if (at < left && left <= at + n[i]) {
+        s.found[0] = tid * BINS + i;
+        s.found[1] = left - at;
+        s.found[2] = left == at + n[i] ? 2u : 1u;
+      }
+      at += n[i];
+    }
+    __syncthreads();
+    const uint32_t how = s.found[2];
+    // all keys below 0xFFFFFFFF are taken, and some of those
+    if (how == 0u) return Cut{0xFFFFFFFFu, left - all};
+    prefix |= s.found[0] << shift;
+    left = s.found[1];
+    top = shift;
+    if (how == 2u) return Cut{prefix | ((1u << shift) - 1u), 0xFFFFFFFFu};
+  }
+  return Cut{prefix, left};
+}
+
+// Places of flagged elements in the order of their numbers: at[i] for element i, and the block's total.
+template <int BLOCK, int PER>
+__device__ uint32_t pick_places(const bool (&flag)[PER], uint32_t (&at)[PER], uint32_t* sums) {
+  const uint32_t wave = threadIdx.x >> 6;
+  uint32_t n = 0;
+  for (int c = 0; c < PER / 4; ++c) {
+    uint32_t below = 0, total = 0;
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t w = __builtin_amdgcn_ballot_w64(flag[4 * c + i]);
+      below += __builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0u));
+      total += (uint32_t)__builtin_popcountll(w);
+    }
+    uint32_t x = n + below;
+    for (int i = 0; i < 4; ++i) {
+      at[4 * c + i] = x;
+      x += flag[4 * c + i] ? 1u : 0u;
+    }
+    n += total;
+  }
+  if ((threadIdx.x & 63u) == 0u) sums[wave] = n;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+  for (uint32_t w = 0; w < BLOCK / 64; ++w) {
+    before += w < wave ? sums[w] : 0u;
+    all += sums[w];
+  }
+  for (int i = 0; i < PER; ++i) at[i] += before;
+  __syncthreads();
+  return all;
+}
+
+// Which elements the cut chooses.
+template <int BLOCK, int PER>
+__device__ void pick_chosen(const uint32_t (&key)[PER], uint32_t count, Cut cut, bool (&out)[PER],
+                            Pick<BLOCK, PER>& s) {
+  for (int i = 0; i < PER; ++i) out[i] = pick_number<BLOCK, PER>(i) < count && key[i] <= cut.key;
+  if (cut.ties == 0xFFFFFFFFu) return;
+  bool tie[PER];
+  uint32_t at[PER];
+  for (int i = 0; i < PER; ++i) tie[i] = out[i] && key[i] == cut.key;
+  const uint32_t ties = pick_places<BLOCK, PER>(tie, at, s.sums[0]);
+  if (ties == cut.ties) return;
+  for (int i = 0; i < PER; ++i) out[i] = out[i] && (!tie[i] || at[i] < cut.ties);
+}
+
+// ------------------------------------------------------------------ victims
+
+// One block per (kv head, sequence) of up to BLOCK * PER entries: weights and positions are read once.
+template <int BLOCK, int PER>
+__global__ __launch_bounds__(BLOCK) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
+                                                           uint32_t recent, uint32_t max_evict,
+                                                           int32_t* victims, int32_t* src, int32_t* new_len) {
+  __shared__ Pick<BLOCK, PER> s;
+  const uint32_t h = blockIdx.x, seq = blockIdx.y, tid = threadIdx.x;
+  a.tok = nullptr;
+  const KvSeq q = kv_seq(a, seq);
+  const uint32_t len = (uint32_t)q.len;
+  uint32_t n = len > budget ? len - budget : 0u;
+  n = n < max_evict ? n : max_evict;
+  const uint32_t stay = len - n;
+  if (h == 0 && tid == 0) new_len[seq] = (int32_t)stay;
+  const size_t row = ((size_t)seq * a.n_kv + h) * max_evict;
+  uint32_t got = 0, moved = 0;
+  if (n) {
+    uint32_t key[PER];
+    int32_t pos[PER];
+    int32_t top = INT32_MIN;
+    for (int c = 0; c < PER / 4; ++c) {
+      const uint32_t e = pick_number<BLOCK, PER>(4 * c);
+      const int32_t p = e < len ? kv_page(a, q, (int32_t)(e >> a.page_bits)) : -1;
+      f32x4 w = (f32x4)0.0f;
+      i32x4 x = (i32x4)0;
+      if (p >= 0) {
+        const size_t at = kv_word(a, p, h) + (e & (a.page - 1u));
+        w = *(const f32x4*)(a.weight + at);
+        x = *(const i32x4*)(a.pos + at);
+      }
+      for (int i = 0; i < 4; ++i) {
+        const bool in = p >= 0 && e + i < len;
+        key[4 * c + i] = in ? kv_order(w[i]) : 0xFFFFFFFFu;
+        pos[4 * c + i] = x[i];
+        if (in) top = x[i] > top ? x[i] : top;
+      }
+    }
+    for (int o = 32; o; o >>= 1) {
+      const int32_t y = __shfl_xor(top, o);
+      top = y > top ? y : top;
+    }
+    if ((tid & 63u) == 0u) s.sums[1][tid >> 6] = (uint32_t)top;
+    __syncthreads();
+    for (uint32_t w = 0; w < BLOCK / 64; ++w) top = (int32_t)s.sums[1][w] > top ? (int32_t)s.sums[1][w] : top;
+    const int64_t newest = (int64_t)top - (int64_t)recent;
+    for (int i = 0; i < PER; ++i)
+      if (pos[i] < (int64_t)first || pos[i] > newest) key[i] = 0xFFFFFFFFu;
+    const Cut cut = pick_cut<BLOCK, PER>(key, n, s);
+    bool out[PER], fill[PER];
+    uint32_t at[PER];
+    pick_chosen<BLOCK, PER>(key, len, cut, out, s);
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t e = pick_number<BLOCK, PER>(i);
+      fill[i] = e >= stay && e < len && !out[i];
+    }
+    got = pick_places<BLOCK, PER>(out, at, s.sums[0]);
+    for (int i = 0; i < PER; ++i)
+      if (out[i]) victims[row + at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
+    moved = pick_places<BLOCK, PER>(fill, at, s.sums[0]);
+    for (int i = 0; i < PER; ++i)
+      if (fill[i]) src[row + at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
+  }
+  for (uint32_t i = got + tid; i < max_evict; i += BLOCK) victims[row + i] = -1;
+  for (uint32_t i = moved + tid; i < max_evict; i += BLOCK) src[row + i] = -1;
+}
+
+// Longer sequences than a block's registers hold are read again in every pass.
+constexpr uint32_t kSelBlock = 1024;
 
 // Inclusive sum over the block of a word per thread; `total` is the block's.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* lds, uint32_t& total) {
@@ -98,11 +390,6 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* lds, uint32
   __syncthreads();
   return x + before;
 }
-
-struct Cut {
-  uint32_t key;   // the largest chosen key
-  uint32_t ties;  // how many entries with that key are chosen: the lowest slots
-};
 
 // The cut below which lie the `need` smallest of key(0) .. key(count - 1), 1 <= need <= count: four
 // passes of 8 bits, each a histogram (of whole numbers: any order gives the same) and its prefix.
@@ -161,7 +448,7 @@ struct WeightKey {
   }
 };
 
-__global__ __launch_bounds__(kSelBlock) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
+__global__ __launch_bounds__(kSelBlock) void kv_victims_long_kernel(KvArgs a, uint32_t budget, uint32_t first,
                                                                uint32_t recent, uint32_t max_evict,
                                                                int32_t* victims, int32_t* src,
                                                                int32_t* new_len) {
@@ -220,46 +507,98 @@ __global__ __launch_bounds__(kSelBlock) void kv_victims_kernel(KvArgs a, uint32_
   for (uint32_t i = moved + tid; i < max_evict; i += kSelBlock) src[row + i] = -1;
 }
 
-// A block per (16 moves, kv head, sequence), a move per 16 threads.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void kv_compact_kernel(KvArgs a, uint32_t max_evict,
-                                                            const int32_t* victims, const int32_t* src,
-                                                            const int32_t* new_len) {
-  const uint32_t h = blockIdx.y, s = blockIdx.z;
-  const uint32_t i = blockIdx.x * (kBlock / 16) + (threadIdx.x >> 4), sub = threadIdx.x & 15u;
-  if (i >= max_evict) return;
+// ------------------------------------------------------------------ compact
+
+// Where the moves of a block read and write; -1: no move.
+struct Move {
+  int64_t from, to;   // first elements of the two pages' keys and values
+  uint32_t sf, st;    // their slots
+};
+
+__device__ __forceinline__ Move move_of(const KvArgs& a, uint32_t h, uint32_t s, uint32_t i, uint32_t max_evict,
+                                        const int32_t* victims, const int32_t* src, const int32_t* new_len) {
+  Move m = {-1, -1, 0, 0};
+  if (i >= max_evict) return m;
   KvArgs b = a;
   b.tok = nullptr;
   const KvSeq q = kv_seq(b, s);
   const int32_t stay = new_len[s];
   const size_t row = ((size_t)s * a.n_kv + h) * max_evict;
   const int32_t from = src[row + i], to = victims[row + i];
-  if (to < 0 || to >= stay || from < stay || from >= q.len) return;
+  if (to < 0 || to >= stay || from < stay || from >= q.len) return m;
   const int32_t pf = kv_page(a, q, from >> a.page_bits), pt = kv_page(a, q, to >> a.page_bits);
-  if (pf < 0 || pt < 0) return;
-  const uint32_t sf = (uint32_t)from & (a.page - 1u), st = (uint32_t)to & (a.page - 1u);
-  const T *kf = (const T*)a.k + kv_base(a, pf, h), *vf = (const T*)a.v + kv_base(a, pf, h);
-  T *kt = (T*)a.k + kv_base(a, pt, h), *vt = (T*)a.v + kv_base(a, pt, h);
-  for (uint32_t d = sub; d < a.dim; d += 16u) {
-    kt[(size_t)st * a.dim + d] = kf[(size_t)sf * a.dim + d];
-    vt[(size_t)d * a.page + st] = vf[(size_t)d * a.page + sf];
+  if (pf < 0 || pt < 0) return m;
+  m.from = (int64_t)kv_base(a, pf, h);
+  m.to = (int64_t)kv_base(a, pt, h);
+  m.sf = (uint32_t)from & (a.page - 1u);
+  m.st = (uint32_t)to & (a.page - 1u);
+  return m;
+}
+
+// Few moves (a step that evicts an entry or two): 64 lanes each, a lane per dimension of the values.
+template <int D>
+__global__ __launch_bounds__(kBlock) void kv_compact_few_kernel(KvArgs a, uint32_t max_evict,
+                                                                const int32_t* victims, const int32_t* src,
+                                                                const int32_t* new_len) {
+  const uint32_t h = blockIdx.y, lane = threadIdx.x & 63u;
+  const Move m = move_of(a, h, blockIdx.z, blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6), max_evict, victims, src,
+                         new_len);
+  if (m.from < 0) return;
+  uint16_t *k = (uint16_t*)a.k, *v = (uint16_t*)a.v;
+  if (lane < D / 8) *(u32x4*)(k + m.to + m.st * D + 8 * lane) = *(const u32x4*)(k + m.from + m.sf * D + 8 * lane);
+  uint16_t x[D / 64];
+  for (uint32_t i = 0; i < D / 64; ++i) x[i] = v[m.from + (size_t)(64 * i + lane) * a.page + m.sf];
+  for (uint32_t i = 0; i < D / 64; ++i) v[m.to + (size_t)(64 * i + lane) * a.page + m.st] = x[i];
+  if (lane == 0) {
+    if (a.weight) a.weight[m.to / D + m.st] = a.weight[m.from / D + m.sf];
+    if (a.pos) a.pos[m.to / D + m.st] = a.pos[m.from / D + m.sf];
   }
-  if (sub == 0) {
-    if (a.weight) a.weight[kv_word(a, pt, h) + st] = a.weight[kv_word(a, pf, h) + sf];
-    if (a.pos) a.pos[kv_word(a, pt, h) + st] = a.pos[kv_word(a, pf, h) + sf];
+}
+
+// Many moves: 64 of a block, whose places lie close together, with a lane per move for the values, so
+// that a load takes its 64 slots of a dimension from a few lines.
+template <int D>
+__global__ __launch_bounds__(kBlock) void kv_compact_kernel(KvArgs a, uint32_t max_evict,
+                                                            const int32_t* victims, const int32_t* src,
+                                                            const int32_t* new_len) {
+  constexpr uint32_t CH = D / 8;
+  __shared__ Move moves[64];
+  const uint32_t h = blockIdx.y, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+  if (tid < 64u) moves[tid] = move_of(a, h, blockIdx.z, blockIdx.x * 64u + tid, max_evict, victims, src, new_len);
+  __syncthreads();
+  uint16_t *k = (uint16_t*)a.k, *v = (uint16_t*)a.v;
+  u32x4 x[CH / 4];
+  for (uint32_t i = 0; i < CH / 4; ++i) {
+    const Move m = moves[(i * kBlock + tid) / CH];
+    if (m.from >= 0) x[i] = *(const u32x4*)(k + m.from + m.sf * D + 8 * (tid % CH));
   }
+  for (uint32_t i = 0; i < CH / 4; ++i) {
+    const Move m = moves[(i * kBlock + tid) / CH];
+    if (m.from >= 0) *(u32x4*)(k + m.to + m.st * D + 8 * (tid % CH)) = x[i];
+  }
+  const Move m = moves[lane];
+  if (m.from < 0) return;
+  const uint16_t* vf = v + m.from + m.sf + (size_t)(wave * (D / 4)) * a.page;
+  uint16_t* vt = v + m.to + m.st + (size_t)(wave * (D / 4)) * a.page;
+  for (uint32_t d = 0; d < D / 4; d += 16) {
+    uint16_t y[16];
+    for (uint32_t i = 0; i < 16; ++i) y[i] = vf[(size_t)(d + i) * a.page];
+    for (uint32_t i = 0; i < 16; ++i) vt[(size_t)(d + i) * a.page] = y[i];
+  }
+  if (wave == 0 && a.weight) a.weight[m.to / D + m.st] = a.weight[m.from / D + m.sf];
+  if (wave == 1 && a.pos) a.pos[m.to / D + m.st] = a.pos[m.from / D + m.sf];
 }
 
 // The boxes after the moves: a block per (page ordinal, kv head, sequence); renewed are the pages
 // below new_len that hold a victim's place or a new end.
-template <typename T>
+template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void kv_rebox_kernel(KvArgs a, uint32_t max_evict,
                                                           const int32_t* victims, const int32_t* new_len) {
-  __shared__ float lds[kBlock / 64];
-  const uint32_t h = blockIdx.y, s = blockIdx.z;
-  KvArgs b = a;
-  b.tok = nullptr;
-  const KvSeq q = kv_seq(b, s);
+  constexpr uint32_t CH = D / 8, RG = kBlock / CH;
+  __shared__ float lds[16 * kBlock];
+  const uint32_t h = blockIdx.y, s = blockIdx.z, c = threadIdx.x % CH, g = threadIdx.x / CH;
+  a.tok = nullptr;
+  const KvSeq q = kv_seq(a, s);
   const int32_t stay = new_len[s] < q.len ? new_len[s] : q.len;
   const int32_t lo = (int32_t)(blockIdx.x << a.page_bits), hi = lo + (int32_t)a.page;
   if (lo >= stay) return;
@@ -274,67 +613,98 @@ __global__ __launch_bounds__(kBlock) void kv_rebox_kernel(KvArgs a, uint32_t max
   }
   const bool got = l < max_evict && v[l] >= lo && v[l] < hi, cut = stay < q.len && stay < hi;
   if (!got && !cut) return;
-  renew_box<T>(a, page, h, stay < hi ? stay - lo : (int32_t)a.page, lds);
+  const int32_t live = stay < hi ? stay - lo : (int32_t)a.page;
+  const uint16_t* k = (const uint16_t*)a.k + kv_base(a, page, h) + 8 * c;
+  Sides side;
+  side.clear();
+  for (int32_t x = (int32_t)g; x < live; x += (int32_t)RG) side.add<T>(*(const u16x8*)(k + (size_t)x * D));
+  write_box<D>(a, page, h, side, lds);
 }
 
 // ------------------------------------------------------------------ the pages of sparse attention
 
-// Keys of the pages for one token and kv head: a block each.  keys [n_tok][n_kv][max_pages], a
-// larger score a smaller key; 0: taken in any case, 0xFFFFFFFF: not there.
-template <typename T>
+constexpr uint32_t kScorePages = 64;  // of a block, 16 a wavefront
+
+// Keys of 64 pages for one token and kv head.  keys [n_tok][n_kv][max_pages], a larger score a smaller
+// key; 0: taken in any case, 0xFFFFFFFF: not there.
+//   sum over heads and dimensions of max(qi lower, qi upper)
+//     = sum over dimensions of (sum over heads of min(qi, 0)) lower + (sum over heads of max(qi, 0)) upper,
+// one product with the box's bytes for all heads of the group.  The summed query has up to 15 bits: two
+// 7-bit halves, so that the products are byte dot products.  Bound by the boxes' bytes.
+template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, uint32_t first, uint32_t last,
                                                           uint32_t* keys) {
-  __shared__ int32_t neg[256], plus[256];
+  constexpr uint32_t LP = 2 * D / 16, PP = 64 / LP;  // lanes of a page, pages of a wavefront's load
+  __shared__ alignas(16) uint8_t half[2][2 * D];     // low and high 7 bits: D of the lower side, D of the upper
   __shared__ float lds[kBlock / 64];
-  const uint32_t h = blockIdx.y, j = blockIdx.x, tid = threadIdx.x;
+  const uint32_t h = blockIdx.y, tid = threadIdx.x, lane = tid & 63u;
+  const uint32_t chunks = (a.max_len + a.page * kScorePages - 1) / (a.page * kScorePages);
+  const uint32_t j = blockIdx.x / chunks, base = (blockIdx.x % chunks) * kScorePages;
   const KvSeq q = kv_seq(a, blockIdx.z);
   if ((int32_t)j >= q.n) return;
   const size_t t = (size_t)q.t0 + j;
   const int32_t limit = q.len - q.n + (int32_t)j + 1;
   const int32_t count = limit > 0 ? (limit + (int32_t)a.page - 1) >> a.page_bits : 0;
-  const T* row = (const T*)nq.p + t * nq.tok + (size_t)h * a.group * nq.head;
+  if ((int32_t)base >= count) return;
+  // the wavefront's 16 pages
+  const int32_t mine = (int32_t)(base + (tid >> 6) * (kScorePages / 4) + (lane & 15u));
+  const int32_t page = mine < count ? kv_page(a, q, mine) : -1;
+  const uint16_t* row = (const uint16_t*)nq.p + t * nq.tok + (size_t)h * a.group * nq.head;
   float top = 0.0f;
-  for (uint32_t i = tid; i < a.group * a.dim; i += kBlock)
-    top = fmaxf(top, fabsf(to_f32(row[(size_t)(i / a.dim) * nq.head + i % a.dim])));
+  for (uint32_t i = tid; i < a.group * D; i += kBlock)
+    top = fmaxf(top, fabsf(bits_f32<T>(row[(size_t)(i / D) * nq.head + i % D])));
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if ((tid & 63u) == 0u) lds[tid >> 6] = top;
   __syncthreads();
-  for (uint32_t w = 0; w < kBlock / 64; ++w) top = fmaxf(top, lds[w]);
+  top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
   const float inv = kv_step(top).inv;
-  if (tid < a.dim) {
+  if (tid < D) {
     int32_t n = 0, p = 0;
     for (uint32_t g = 0; g < a.group; ++g) {
-      const int32_t x = kv_clip(rintf(to_f32(row[(size_t)g * nq.head + tid]) * inv));
-      n += x < 0 ? x : 0;
+      const int32_t x = kv_clip(rintf(bits_f32<T>(row[(size_t)g * nq.head + tid]) * inv));
+      n -= x < 0 ? x : 0;
       p += x > 0 ? x : 0;
     }
-    neg[tid] = n;
-    plus[tid] = p;
+    half[0][tid] = (uint8_t)(n & 127);
+    half[1][tid] = (uint8_t)(n >> 7);
+    half[0][D + tid] = (uint8_t)(p & 127);
+    half[1][D + tid] = (uint8_t)(p >> 7);
   }
   __syncthreads();
-  uint32_t* out = keys + (t * a.n_kv + h) * a.max_pages;
-  for (int32_t o = (int32_t)tid; o < count; o += (int32_t)kBlock) {
-    const int32_t page = kv_page(a, q, o);
-    uint32_t key = 0xFFFFFFFFu;
-    if (page >= 0) {
-      if (o < (int32_t)first || o >= count - (int32_t)last) {
-        key = 0;
-      } else {
-        const size_t at = (size_t)page * a.n_kv + h;
-        const int8_t* b = a.box + at * 2 * a.dim;
-        int32_t sum = 0;
-        for (uint32_t d = 0; d < a.dim; ++d) sum += neg[d] * b[d] + plus[d] * b[a.dim + d];
-        key = ~kv_order((float)sum * a.box_scale[at]);
-      }
-    }
-    out[o] = key;
+  const uint32_t sub = lane % LP;
+  const i32x4 ql = *(const i32x4*)&half[0][16 * sub], qh = *(const i32x4*)&half[1][16 * sub];
+  i32x4 b[16 / PP];
+  for (uint32_t i = 0; i < 16 / PP; ++i) {
+    const int32_t p = __shfl(page, (int)(i * PP + lane / LP));
+    b[i] = (i32x4)0;
+    if (p >= 0) b[i] = *(const i32x4*)(a.box + ((size_t)p * a.n_kv + h) * 2 * D + 16 * sub);
   }
+  int32_t score = 0;  // of page `mine`, in lanes 0 to 15
+  for (uint32_t i = 0; i < 16 / PP; ++i) {
+    int32_t x = 0, y = 0;
+    for (int w = 0; w < 4; ++w) {
+      x = __builtin_amdgcn_sdot4(ql[w], b[i][w], x, false);
+      y = __builtin_amdgcn_sdot4(qh[w], b[i][w], y, false);
+    }
+    x += y * 128;
+    x = sub < LP / 2 ? -x : x;
+    for (uint32_t o = LP / 2; o; o >>= 1) x += __shfl_xor(x, (int)o);
+    // lane l of 0 to 15 takes page l, which lanes (l % PP) LP have in step l / PP
+    const int32_t got = __shfl(x, (int)((lane % PP) * LP));
+    score = (lane & 15u) / PP == i ? got : score;
+  }
+  if (lane >= 16u || mine >= count) return;
+  uint32_t key = 0xFFFFFFFFu;
+  if (page >= 0)
+    key = mine < (int32_t)first || mine >= count - (int32_t)last
+              ? 0u : ~kv_order((float)score * a.box_scale[(size_t)page * a.n_kv + h]);
+  keys[(t * a.n_kv + h) * a.max_pages + (uint32_t)mine] = key;
 }
 
-__global__ __launch_bounds__(kBlock) void kv_choose_kernel(KvArgs a, uint32_t n_sel, const uint32_t* keys,
-                                                           int32_t* sel) {
-  __shared__ uint32_t hist[258];
-  __shared__ uint32_t scan[kBlock / 64];
+template <int BLOCK, int PER>
+__global__ __launch_bounds__(BLOCK) void kv_choose_kernel(KvArgs a, uint32_t n_sel, const uint32_t* keys,
+                                                          int32_t* sel) {
+  __shared__ Pick<BLOCK, PER> s;
   const uint32_t h = blockIdx.y, j = blockIdx.x, tid = threadIdx.x;
   const KvSeq q = kv_seq(a, blockIdx.z);
   if ((int32_t)j >= q.n) return;
@@ -343,24 +713,58 @@ __global__ __launch_bounds__(kBlock) void kv_choose_kernel(KvArgs a, uint32_t n_
   const uint32_t count = limit > 0 ? (uint32_t)(limit + (int32_t)a.page - 1) >> a.page_bits : 0u;
   const uint32_t* in = keys + (t * a.n_kv + h) * a.max_pages;
   int32_t* out = sel + (t * a.n_kv + h) * n_sel;
-  const uint32_t need = n_sel < count ? n_sel : count;
   uint32_t got = 0;
-  if (need) {
-    const Cut cut = smallest(count, need, [&](uint32_t i) { return in[i]; }, hist);
-    uint32_t ties = 0;
-    for (uint32_t base = 0; base < count; base += kBlock) {
-      const uint32_t o = base + tid, x = o < count ? in[o] : 0xFFFFFFFFu;
-      uint32_t total;
-      const uint32_t tie = o < count && x == cut.key ? 1u : 0u;
-      const uint32_t rank = ties + block_scan(tie, scan, total) - tie;
-      ties += total;
-      const uint32_t take = x != 0xFFFFFFFFu && (x < cut.key || (tie && rank < cut.ties)) ? 1u : 0u;
-      const uint32_t at = block_scan(take, scan, total);
-      if (take) out[got + at - 1u] = (int32_t)o;
-      got += total;
+  if (count) {
+    uint32_t key[PER];
+    bool take[PER];
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t o = pick_number<BLOCK, PER>(i);
+      key[i] = o < count ? in[o] : 0xFFFFFFFFu;
     }
+    if (count > n_sel) {
+      const Cut cut = pick_cut<BLOCK, PER>(key, n_sel, s);
+      pick_chosen<BLOCK, PER>(key, count, cut, take, s);
+    }
+    for (int i = 0; i < PER; ++i) take[i] = (count <= n_sel || take[i]) && key[i] != 0xFFFFFFFFu;
+    uint32_t at[PER];
+    got = pick_places<BLOCK, PER>(take, at, s.sums[0]);
+    for (int i = 0; i < PER; ++i)
+      if (take[i]) out[at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
   }
-  for (uint32_t i = got + tid; i < n_sel; i += kBlock) out[i] = -1;
+  for (uint32_t i = got + tid; i < n_sel; i += BLOCK) out[i] = -1;
+}
+
+}  // namespace
+
+namespace {
+
+template <typename F>
+hipError_t with_dim(uint32_t dim, F f) {
+  if (dim == 64) f(std::integral_constant<int, 64>{});
+  else if (dim == 128) f(std::integral_constant<int, 128>{});
+  else f(std::integral_constant<int, 256>{});
+  return hipGetLastError();
+}
+
+template <typename F>
+hipError_t with_type(const KvArgs& a, F f) {
+  return with_dim(a.dim, [&](auto d) {
+    if (a.dtype == UNISON_KV_BF16) f(__hip_bfloat16{}, d);
+    else f(__half{}, d);
+  });
+}
+
+// The smallest block whose registers hold `n` keys: fewer wavefronts meet at fewer barriers, and more
+// blocks fit a compute unit.
+template <typename F>
+bool with_pick(uint32_t n, F f) {
+  if (n <= 1024) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  else if (n <= 4096) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
+  else if (n <= 8192) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{});
+  else if (n <= 16384) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16>{});
+  else if (n <= 32768) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 32>{});
+  else return false;
+  return true;
 }
 
 }  // namespace
@@ -369,48 +773,59 @@ hipError_t launch_kv_append(const KvArgs& a, const KvRows& k, const KvRows& v, c
                             hipStream_t st) {
   const uint32_t most = a.max_new < a.max_len ? a.max_new : a.max_len;
   const dim3 grid((most + 2 * a.page - 2) / a.page, a.n_kv, a.n_seq);
-  if (a.dtype == UNISON_KV_BF16)
-    hipLaunchKernelGGL(kv_append_kernel<__hip_bfloat16>, grid, dim3(kBlock), 0, st, a, k, v, pos);
-  else
-    hipLaunchKernelGGL(kv_append_kernel<__half>, grid, dim3(kBlock), 0, st, a, k, v, pos);
-  return hipGetLastError();
+  return with_type(a, [&](auto t, auto d) {
+    hipLaunchKernelGGL((kv_append_kernel<decltype(t), decltype(d)::value>), grid, dim3(kBlock), 0, st, a, k, v, pos);
+  });
 }
 
 hipError_t launch_kv_victims(const KvArgs& a, uint32_t budget, uint32_t first, uint32_t recent,
                              uint32_t max_evict, int32_t* victims, int32_t* src, int32_t* new_len,
                              hipStream_t st) {
-  hipLaunchKernelGGL(kv_victims_kernel, dim3(a.n_kv, a.n_seq), dim3(kSelBlock), 0, st, a, budget, first, recent,
-                     max_evict, victims, src, new_len);
+  const dim3 grid(a.n_kv, a.n_seq);
+  if (!with_pick(a.max_len, [&](auto block, auto per) {
+        hipLaunchKernelGGL((kv_victims_kernel<decltype(block)::value, decltype(per)::value>), grid,
+                           dim3(decltype(block)::value), 0, st, a, budget, first, recent, max_evict, victims, src,
+                           new_len);
+      }))
+    hipLaunchKernelGGL(kv_victims_long_kernel, grid, dim3(kSelBlock), 0, st, a, budget, first, recent, max_evict,
+                       victims, src, new_len);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_compact(const KvArgs& a, uint32_t max_evict, const int32_t* victims, const int32_t* src,
                              const int32_t* new_len, hipStream_t st) {
-  const dim3 grid((max_evict + kBlock / 16 - 1) / (kBlock / 16), a.n_kv, a.n_seq);
+  // a lane per move pays once a block has 16 of its 64 moves
+  const bool few = max_evict < 16;
+  const uint32_t per = few ? kBlock / 64 : 64;
+  const dim3 grid((max_evict + per - 1) / per, a.n_kv, a.n_seq);
   const dim3 pages((a.max_len + a.page - 1) / a.page, a.n_kv, a.n_seq);
-  if (a.dtype == UNISON_KV_BF16) {
-    hipLaunchKernelGGL(kv_compact_kernel<__hip_bfloat16>, grid, dim3(kBlock), 0, st, a, max_evict, victims, src,
-                       new_len);
+  return with_type(a, [&](auto t, auto d) {
+    constexpr int D = decltype(d)::value;
+    if (few)
+      hipLaunchKernelGGL(kv_compact_few_kernel<D>, grid, dim3(kBlock), 0, st, a, max_evict, victims, src, new_len);
+    else
+      hipLaunchKernelGGL(kv_compact_kernel<D>, grid, dim3(kBlock), 0, st, a, max_evict, victims, src, new_len);
     if (a.box)
-      hipLaunchKernelGGL(kv_rebox_kernel<__hip_bfloat16>, pages, dim3(kBlock), 0, st, a, max_evict, victims,
+      hipLaunchKernelGGL((kv_rebox_kernel<decltype(t), D>), pages, dim3(kBlock), 0, st, a, max_evict, victims,
                          new_len);
-  } else {
-    hipLaunchKernelGGL(kv_compact_kernel<__half>, grid, dim3(kBlock), 0, st, a, max_evict, victims, src, new_len);
-    if (a.box)
-      hipLaunchKernelGGL(kv_rebox_kernel<__half>, pages, dim3(kBlock), 0, st, a, max_evict, victims, new_len);
-  }
-  return hipGetLastError();
+  });
 }
 
 hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, uint32_t n_sel, uint32_t first, uint32_t last,
                             uint32_t* keys, int32_t* sel, hipStream_t st) {
-  const dim3 grid(a.max_new, a.n_kv, a.n_seq);
-  if (a.dtype == UNISON_KV_BF16)
-    hipLaunchKernelGGL(kv_score_kernel<__hip_bfloat16>, grid, dim3(kBlock), 0, st, a, q, first, last, keys);
-  else
-    hipLaunchKernelGGL(kv_score_kernel<__half>, grid, dim3(kBlock), 0, st, a, q, first, last, keys);
-  hipLaunchKernelGGL(kv_choose_kernel, grid, dim3(kBlock), 0, st, a, n_sel, (const uint32_t*)keys, sel);
-  return hipGetLastError();
+  const uint32_t pages = (a.max_len + a.page - 1) / a.page;
+  const dim3 grid(a.max_new * ((pages + kScorePages - 1) / kScorePages), a.n_kv, a.n_seq);
+  const hipError_t rc = with_type(a, [&](auto t, auto d) {
+    hipLaunchKernelGGL((kv_score_kernel<decltype(t), decltype(d)::value>), grid, dim3(kBlock), 0, st, a, q, first, last,
+                       keys);
+  });
+  if (rc != hipSuccess) return rc;
+  const bool fits = with_pick(pages, [&](auto block, auto per) {
+    hipLaunchKernelGGL((kv_choose_kernel<decltype(block)::value, decltype(per)::value>),
+                       dim3(a.max_new, a.n_kv, a.n_seq), dim3(decltype(block)::value), 0, st, a, n_sel,
+                       (const uint32_t*)keys, sel);
+  });
+  return fits ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 }  // namespace unison
