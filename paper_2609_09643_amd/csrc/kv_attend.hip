@@ -69,7 +69,7 @@ struct Attn {
   // index ((split * n_seq + s) * n_kv + h) * row_cap + r
   float* part_o;        // [..][dim], times the exponential of the maximum
   float2* part_ml;      // maximum (power of two) and sum
-  float* scores;        // [n_seq][n_kv][row_cap][score_len], or null
+  float* scores;        // of the dense few-rows kernel (score_at), or null
   uint32_t n_split, chunk, row_cap, score_len;
   uint32_t rows_from, rows_to;  // rows of a sequence that this launch serves: rows_from < n * group <= rows_to
 };
@@ -79,6 +79,14 @@ __device__ __forceinline__ float or_zero(float m) { return m == -kInf ? 0.0f : m
 
 __device__ __forceinline__ size_t part_row(const Attn& p, uint32_t split, uint32_t s, uint32_t h) {
   return (((size_t)split * p.a.n_seq + s) * p.a.n_kv + h) * p.row_cap;
+}
+
+// Scores of row r and 32 entries, those 8 g + 4 x to + 3 of them in word g: rows side by side, so that the
+// lanes of a store write runs of 64 bytes a row.
+__device__ __forceinline__ f32x4* score_at(const Attn& p, uint32_t s, uint32_t h, uint32_t group32, uint32_t x,
+                                           uint32_t r) {
+  const size_t unit = (size_t)s * p.a.n_kv + h;
+  return (f32x4*)p.scores + (((unit * (p.score_len / 32) + group32) * 2 + x) * p.row_cap + r) * 4;
 }
 
 template <typename M, int N>
@@ -93,22 +101,24 @@ __device__ __forceinline__ void store4(typename M::t* out, const float (&x)[N]) 
 
 // Attention of up to 16 * NT rows (new tokens x the kv head's query heads) over a chunk of entries:
 // what a decode step is.  It reads every key and value once and computes little on each, so it is
-// bound by HBM; the wavefronts of a block take tiles of 32 entries in turn, straight from memory
-// into the matrix operands, and join their maxima, sums and products in LDS at the end.  With
+// bound by HBM; the wavefronts of a block take runs of 64 entries in turn, straight from memory into
+// the matrix operands, and join their maxima, sums and products in LDS at the end.  64 entries of a
+// dimension are a line of V (of 128 bytes): with 32 a wavefront, two of them fetched every line.  With
 // SPARSE a block serves one token and reads the pages of its choice instead of all.
 template <typename M, int D, int NT, bool SPARSE, bool SCORES>
-__global__ __launch_bounds__(kBlock, NT * D <= 128 ? 3 : NT * D <= 256 ? 2 : 1) void kv_few_kernel(Attn p) {
+__global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(Attn p) {
   typedef typename M::t T;
   typedef typename M::v8 v8;
-  constexpr int KS = D / 32, DT = D / 16;
-  __shared__ int32_t pg[kPagesLds + 1];
-  __shared__ int32_t eb[SPARSE ? kPagesLds + 1 : 1];
+  // H groups of 32 entries an iteration; wide heads or two row tiles leave registers for one, two in a row
+  constexpr int KS = D / 32, DT = D / 16, H = NT * D > 128 ? 1 : 2;
+  __shared__ int32_t pg[kPagesLds + 4];
+  __shared__ int32_t eb[SPARSE ? kPagesLds + 4 : 1];
   __shared__ f32x4 join[(kWaves / 2) * NT * DT * 64];
   __shared__ float2 join_ml[(kWaves / 2) * NT * 64];
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 63u;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
-  const uint32_t split = blockIdx.x % p.n_split;
+  const uint32_t split = spread_piece(blockIdx.x % p.n_split, p.n_split);
   const KvSeq q = kv_seq(a, s);
   uint32_t r0 = 0, rows;
   const int32_t* sel = nullptr;
@@ -127,7 +137,8 @@ __global__ __launch_bounds__(kBlock, NT * D <= 128 ? 3 : NT * D <= 256 ? 2 : 1) 
   const uint32_t start = split * p.chunk, end = start + p.chunk < all ? start + p.chunk : all;
   if (start >= all && split) return;
 
-  for (uint32_t i = tid; i < (p.chunk >> a.page_bits) + 1u; i += kBlock) {
+  // a run of 64 may end past the chunk: up to three pages more, which are not there
+  for (uint32_t i = tid; i < (p.chunk >> a.page_bits) + 4u; i += kBlock) {
     int32_t page = -1, o = -1;
     if (start + (i << a.page_bits) < end) {
       o = (int32_t)((start >> a.page_bits) + i);
@@ -167,56 +178,70 @@ __global__ __launch_bounds__(kBlock, NT * D <= 128 ? 3 : NT * D <= 256 ? 2 : 1) 
   }
   const size_t head = (size_t)h * a.page * D, per_page = (size_t)a.n_kv * a.page * D;
   const uint32_t in_page = a.page - 1u;
-  // keys: lane r of the left operand has entry 8 (r / 4) + r % 4 of the tile, and 4 behind it
+  // keys: lane r of the left operand has entry 8 (r / 4) + r % 4 of a group, and 4 behind it
   const uint32_t k_of = 8u * (r16 >> 2);
-  const auto load_k = [&](uint32_t i, v8 (&k)[2][KS]) {
-    const uint32_t e = i + k_of;
-    int32_t page = pg[(e - start) >> a.page_bits];
-    page = page < 0 ? 0 : page;
-    const T* at = (const T*)a.k + (size_t)page * per_page + head + ((e & in_page) + (r16 & 3u)) * D + 8 * g4;
-    for (int x = 0; x < 2; ++x)
-      for (int c = 0; c < KS; ++c) k[x][c] = *(const v8*)(at + x * 4 * D + 32 * c);
-  };
-  v8 k[2][KS];
-  uint32_t i = start + 32u * wave;
-  if (i < end) load_k(i, k);
-  for (; i < end; i += 32u * kWaves) {
-    // values: lane r has dimension r of each 16, entries 8 (lane / 16) to + 7
-    v8 v[DT];
-    const uint32_t ev = i + 8u * g4;
-    const int32_t vpage = pg[(ev - start) >> a.page_bits];
-    {
-      const T* at = (const T*)a.v + (size_t)(vpage < 0 ? 0 : vpage) * per_page + head + (size_t)r16 * a.page +
-                    (ev & in_page);
-      for (int t = 0; t < DT; ++t) v[t] = *(const v8*)(at + (size_t)t * 16 * a.page);
+  const auto load_k = [&](uint32_t i, v8 (&k)[H][2][KS]) {
+    for (int y = 0; y < H; ++y) {
+      const uint32_t e = i + 32u * y + k_of;
+      int32_t page = pg[(e - start) >> a.page_bits];
+      page = page < 0 ? 0 : page;
+      const T* at = (const T*)a.k + (size_t)page * per_page + head + ((e & in_page) + (r16 & 3u)) * D + 8 * g4;
+      for (int x = 0; x < 2; ++x)
+        for (int c = 0; c < KS; ++c) k[y][x][c] = *(const v8*)(at + x * 4 * D + 32 * c);
     }
-    f32x4 sc[NT][2];
+  };
+  // the wavefront's groups: runs of 64 entries, every kWaves-th
+  const auto after = [&](uint32_t i) {
+    return H == 2 ? i + 64u * kWaves : ((i - start) & 32u) ? i + 64u * kWaves - 32u : i + 32u;
+  };
+  v8 k[H][2][KS];
+  uint32_t i = start + 64u * wave;
+  if (i < end) load_k(i, k);
+  while (i < end) {
+    // values: lane r has dimension r of each 16, entries 8 (lane / 16) to + 7 of a group
+    v8 v[H][DT];
+    int32_t vpage[H], mine[H];
+    bool inside = true;
+    for (int y = 0; y < H; ++y) {
+      const uint32_t ev = i + 32u * y + 8u * g4, at_page = (ev - start) >> a.page_bits;
+      vpage[y] = pg[at_page];
+      // the entry of the lane's first value, and whether every row sees all of them
+      mine[y] = SPARSE ? eb[at_page] + (int32_t)(ev & in_page) : (int32_t)ev;
+      inside = inside && vpage[y] >= 0 && mine[y] + 8 <= seen_by_all;
+      const T* at = (const T*)a.v + (size_t)(vpage[y] < 0 ? 0 : vpage[y]) * per_page + head + (size_t)r16 * a.page +
+                    (ev & in_page);
+      for (int t = 0; t < DT; ++t) v[y][t] = *(const v8*)(at + (size_t)t * 16 * a.page);
+    }
+    f32x4 sc[NT][H][2];
     for (int n = 0; n < NT; ++n)
-      for (int x = 0; x < 2; ++x) {
-        sc[n][x] = (f32x4)0.0f;
-        for (int c = 0; c < KS; ++c) sc[n][x] = M::mma16(k[x][c], qf[n][c], sc[n][x]);
-      }
-    if (i + 32u * kWaves < end) load_k(i + 32u * kWaves, k);
-    // the entry of the lane's first value, and whether every row sees the whole tile
-    const int32_t mine = SPARSE ? eb[(ev - start) >> a.page_bits] + (int32_t)(ev & in_page) : (int32_t)ev;
-    const bool inside = vpage >= 0 && mine + 8 <= seen_by_all;
+      for (int y = 0; y < H; ++y)
+        for (int x = 0; x < 2; ++x) {
+          sc[n][y][x] = (f32x4)0.0f;
+          for (int c = 0; c < KS; ++c) sc[n][y][x] = M::mma16(k[y][x][c], qf[n][c], sc[n][y][x]);
+        }
+    const uint32_t next_i = after(i);
+    if (next_i < end) load_k(next_i, k);
     const bool whole = __builtin_amdgcn_ballot_w64(!inside) == 0ull;
     if (!whole)
-      for (int t = 0; t < DT; ++t)
+      for (int y = 0; y < H; ++y)
         for (int x = 0; x < 8; ++x)  // what is not an entry may hold anything
-          if (vpage < 0 || mine + x >= q.len) v[t][x] = (T)0.0f;
+          if (vpage[y] < 0 || mine[y] + x >= q.len)
+            for (int t = 0; t < DT; ++t) v[y][t][x] = (T)0.0f;
     for (int n = 0; n < NT; ++n) {
-      float z[8];
-      for (int x = 0; x < 8; ++x) z[x] = sc[n][x >> 2][x & 3] * p.scale2;
-      if (!whole)
-        for (int x = 0; x < 8; ++x)
-          if (vpage < 0 || mine + x >= limit[n]) z[x] = -kInf;
-      if (SCORES && r16 + 16u * n < rows) {
-        float* to = p.scores + (((size_t)s * a.n_kv + h) * p.row_cap + r16 + 16u * n) * p.score_len + ev;
-        *(f32x4*)to = f32x4{z[0], z[1], z[2], z[3]};
-        *(f32x4*)(to + 4) = f32x4{z[4], z[5], z[6], z[7]};
+      float z[H][8];
+      float top = -kInf;
+      for (int y = 0; y < H; ++y) {
+        for (int x = 0; x < 8; ++x) z[y][x] = sc[n][y][x >> 2][x & 3] * p.scale2;
+        if (!whole)
+          for (int x = 0; x < 8; ++x)
+            if (vpage[y] < 0 || mine[y] + x >= limit[n]) z[y][x] = -kInf;
+        if (SCORES && r16 + 16u * n < rows) {
+          f32x4* to = score_at(p, s, h, (i >> 5) + y, 0, r16 + 16u * n) + g4;
+          to[0] = f32x4{z[y][0], z[y][1], z[y][2], z[y][3]};
+          to[4u * p.row_cap] = f32x4{z[y][4], z[y][5], z[y][6], z[y][7]};
+        }
+        for (int x = 0; x < 8; ++x) top = fmaxf(top, z[y][x]);
       }
-      float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
       if (__builtin_amdgcn_ballot_w64(top > m[n] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -227,16 +252,19 @@ __global__ __launch_bounds__(kBlock, NT * D <= 128 ? 3 : NT * D <= 256 ? 2 : 1) 
         for (int t = 0; t < DT; ++t) o[n][t] *= f;
       }
       const float base = or_zero(m[n]);
-      v8 pf;
-      for (int x = 0; x < 8; ++x) {
-        const float e = exp2_fast(z[x] - base);
-        l[n] += e;
-        // p is rounded to the inputs' type for the second product (half a step of each term); the sum
-        // it is divided by is not
-        pf[x] = (T)e;
+      for (int y = 0; y < H; ++y) {
+        v8 pf;
+        for (int x = 0; x < 8; ++x) {
+          const float e = exp2_fast(z[y][x] - base);
+          l[n] += e;
+          // p is rounded to the inputs' type for the second product (half a step of each term); the
+          // sum it is divided by is not
+          pf[x] = (T)e;
+        }
+        for (int t = 0; t < DT; ++t) o[n][t] = M::mma16(v[y][t], pf, o[n][t]);
       }
-      for (int t = 0; t < DT; ++t) o[n][t] = M::mma16(v[t], pf, o[n][t]);
     }
+    i = next_i;
   }
   for (int n = 0; n < NT; ++n) {
     l[n] += __shfl_xor(l[n], 16);
@@ -295,17 +323,29 @@ __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
   const uint32_t d = 4 * (threadIdx.x % (D / 4));
   const uint32_t all = p.sel ? p.n_sel << a.page_bits : (uint32_t)q.len;
   const uint32_t used = all ? (all + p.chunk - 1) / p.chunk : 1u;
-  float m = -kInf;
-  for (uint32_t i = 0; i < used; ++i) m = fmaxf(m, p.part_ml[part_row(p, i, s, h) + r].x);
-  const float base = or_zero(m);
-  float l = 0.0f;
+  float m = -kInf, l = 0.0f;
   f32x4 o = (f32x4)0.0f;
-  for (uint32_t i = 0; i < used; ++i) {
-    const size_t part = part_row(p, i, s, h) + r;
-    const float2 y = p.part_ml[part];
-    const float f = exp2_fast(y.x - base);
-    l += y.y * f;
-    o += *(const f32x4*)(p.part_o + part * D + d) * f;
+  for (uint32_t i0 = 0; i0 < used; i0 += 8) {  // eight splits' loads in flight
+    float2 y[8];
+    f32x4 x[8];
+    for (uint32_t i = 0; i < 8; ++i) {
+      const bool is = i0 + i < used;
+      const size_t part = part_row(p, is ? i0 + i : i0, s, h) + r;
+      y[i] = p.part_ml[part];
+      x[i] = *(const f32x4*)(p.part_o + part * D + d);
+      if (!is) y[i] = make_float2(-kInf, 0.0f);
+    }
+    float next = m;
+    for (uint32_t i = 0; i < 8; ++i) next = fmaxf(next, y[i].x);
+    const float base = or_zero(next), f = exp2_fast(m - base);
+    m = next;
+    l *= f;
+    o *= f;
+    for (uint32_t i = 0; i < 8; ++i) {
+      const float g = exp2_fast(y[i].x - base);
+      l += y[i].y * g;
+      o += x[i] * g;
+    }
   }
   const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
   const size_t row = (size_t)(q.t0 + (int32_t)(r / a.group)) * a.n_q + h * a.group + r % a.group;
@@ -322,26 +362,34 @@ __global__ __launch_bounds__(kBlock) void kv_weight_few_kernel(Attn p, float dec
   const uint32_t h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
   const KvSeq q = kv_seq(a, s);
   const uint32_t rows = (uint32_t)q.n * a.group;
-  if (rows == 0 || blockIdx.x * 4 * kBlock >= (uint32_t)q.len) return;
+  const uint32_t piece = spread_piece(blockIdx.x, gridDim.x);
+  if (rows == 0 || piece * 4 * kBlock >= (uint32_t)q.len) return;
   if (tid < rows) {
     const uint32_t used = ((uint32_t)q.len + p.chunk - 1) / p.chunk;
     float m = -kInf, l = 0.0f;
-    for (uint32_t i = 0; i < used; ++i) m = fmaxf(m, p.part_ml[part_row(p, i, s, h) + tid].x);
-    for (uint32_t i = 0; i < used; ++i) {
-      const float2 y = p.part_ml[part_row(p, i, s, h) + tid];
-      l += y.y * exp2_fast(y.x - or_zero(m));
+    for (uint32_t i0 = 0; i0 < used; i0 += 8) {
+      float2 y[8];
+      float next = m;
+      for (uint32_t i = 0; i < 8; ++i) {
+        y[i] = p.part_ml[part_row(p, i0 + i < used ? i0 + i : i0, s, h) + tid];
+        if (i0 + i >= used) y[i] = make_float2(-kInf, 0.0f);
+        next = fmaxf(next, y[i].x);
+      }
+      l *= exp2_fast(m - or_zero(next));
+      m = next;
+      for (uint32_t i = 0; i < 8; ++i) l += y[i].y * exp2_fast(y[i].x - or_zero(m));
     }
     base[tid] = l == 0.0f ? kInf : m + log2f(l);
   }
   __syncthreads();
-  const uint32_t e = 4 * (blockIdx.x * kBlock + tid);
+  const uint32_t e = 4 * (piece * kBlock + tid);
   if (e >= (uint32_t)q.len) return;
   const int32_t page = kv_page(a, q, (int32_t)(e >> a.page_bits));
   if (page < 0) return;
-  const float* z = p.scores + ((size_t)s * a.n_kv + h) * p.row_cap * p.score_len + e;
+  const f32x4* z = score_at(p, s, h, e >> 5, (e >> 2) & 1u, 0) + ((e >> 3) & 3u);
   f32x4 sum = (f32x4)0.0f;
   for (uint32_t r = 0; r < rows; ++r) {
-    const f32x4 x = *(const f32x4*)(z + (size_t)r * p.score_len);
+    const f32x4 x = z[4u * r];
     for (int i = 0; i < 4; ++i) sum[i] += exp2_fast(x[i] - base[r]);
   }
   float* w = a.weight + kv_word(a, page, h) + (e & (a.page - 1u));
@@ -363,15 +411,33 @@ __device__ __forceinline__ uint32_t swap23(uint32_t x) {
   return (x & ~12u) | ((x & 4u) << 1) | ((x & 8u) >> 1);
 }
 
+// Where a row of `CH` 16-byte pieces keeps piece c: xored with the row, so that 16 rows' pieces c, which
+// a read takes at once, lie in different banks (64 banks hold two rows of 8 pieces).
+template <uint32_t CH>
+__device__ __forceinline__ uint32_t spread(uint32_t row) {
+  return CH == 8 ? (row >> 1) & 7u : row & 15u;
+}
+
+// A row of the queries, negated where the scale is negative: the kernels below scale by its magnitude.
+template <typename v8>
+__device__ __forceinline__ v8 signed_row(v8 x, bool negate) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+  const u4 y = __builtin_bit_cast(u4, x) ^ (negate ? 0x80008000u : 0u);
+  return __builtin_bit_cast(v8, y);
+}
+// A scale of 0 would make NaN of the scores that a mask sets to -inf.
+__device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(scale2), 1e-35f); }
+
 // Attention of 128 rows over a chunk of entries, 32 rows a wavefront, 64 entries at a time from
-// double-buffered LDS: a turn's new tokens over their session.  The 16-byte pieces of a row are
-// stored at places xored with the row, so that the 8 or 16 rows that a read takes at once lie in
-// different banks.  Bound by the matrix cores and the exponentials beside them.
+// double-buffered LDS: a turn's new tokens over their session.  Bound by the matrix cores and, nearly as
+// much, by the exponentials (a quarter of the rate) and the additions and roundings beside them, so the
+// two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
+// the second product of the group before and the first product of the group behind.
 template <typename M, int D>
 __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {
   typedef typename M::t T;
   typedef typename M::v8 v8;
-  constexpr uint32_t CH = D / 8, MASK = CH - 1 < 15 ? CH - 1 : 15;
+  constexpr uint32_t CH = D / 8;
   constexpr int KS = D / 16, DT = D / 32, NK = CH / 4, NV = D / 32;
   __shared__ v8 kt[2][kManyKeys * CH];
   __shared__ v8 vt[2][D * 8];
@@ -392,133 +458,203 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
   const auto token = [&](uint32_t x) { return (int32_t)((x < rows ? x : rows - 1u) / a.group); };
   const int32_t block_end = old + token((tile + 1u) * kManyRows - 1u) + 1;
   const uint32_t w0 = tile * kManyRows + 32u * wave;
-  const int32_t wave_end = w0 < rows ? old + token(w0 + 31u) + 1 : 0;
-  const int32_t seen_by_all = old + token(w0) + 1;
   const int32_t start = (int32_t)(split * p.chunk);
-  int32_t end = block_end < q.len ? block_end : q.len;
-  if ((uint32_t)end > (uint32_t)start + p.chunk && end > 0) end = start + (int32_t)p.chunk;
   if (start >= q.len && split) return;
+  int32_t end = block_end < q.len ? block_end : q.len;
+  if (end > 0 && (uint32_t)end > (uint32_t)start + p.chunk) end = start + (int32_t)p.chunk;
+  const int32_t tiles = end > start ? (end - start + 63) >> 6 : 0;
+  const int32_t wave_end = w0 < rows ? old + token(w0 + 31u) + 1 : 0;
+  int32_t wave_tiles = (wave_end < end ? wave_end : end) - start;
+  wave_tiles = wave_tiles > 0 ? (wave_tiles + 63) >> 6 : 0;
+  const int32_t seen_by_all = old + token(w0) + 1;
+  const float scale = magnitude(p.scale2);
 
   v8 qf[KS];
   {
     const T* row = (const T*)p.q.p + (size_t)(q.t0 + (int32_t)j) * p.q.tok + (h * a.group + g) * p.q.head;
+#pragma unroll
     for (int k = 0; k < KS; ++k) {
-      v8 x = *(const v8*)(row + 16 * k + 8 * half);
+      v8 x = signed_row(*(const v8*)(row + 16 * k + 8 * half), p.scale2 < 0.0f);
       if (!is) x = (v8)(T)0.0f;
       qf[k] = x;
     }
   }
   f32x16 o[DT];
+#pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = (f32x16)0.0f;
   float m = -kInf, l = 0.0f;
 
   const size_t head = (size_t)h * a.page * D, per_page = (size_t)a.n_kv * a.page * D;
   const uint32_t in_page = a.page - 1u;
-  // the pages of a tile's four runs of 16 entries; bit 4 i of the result: run i is there
-  int32_t pg[4];
-  const auto pages_of = [&](int32_t base, int32_t (&to)[4]) {
-    for (int i = 0; i < 4; ++i) {
-      const int32_t e = base + 16 * i;
-      to[i] = e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
-    }
+  struct Pages {  // of a tile's four runs of 16 entries
+    int32_t x[4];
   };
-  const auto pick = [&](const int32_t (&from)[4], uint32_t i) {
-    const int32_t x = i & 1u ? from[1] : from[0], y = i & 1u ? from[3] : from[2];
+  const auto pages_of = [&](int32_t t) {
+    Pages to;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t e = start + 64 * t + 16 * i;
+      to.x[i] = t < tiles && e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
+    }
+    return to;
+  };
+  const auto pick = [&](const Pages& from, uint32_t i) {
+    const int32_t x = i & 1u ? from.x[1] : from.x[0], y = i & 1u ? from.x[3] : from.x[2];
     const int32_t z = i & 2u ? y : x;
     return z < 0 ? 0 : z;
   };
-  const auto load = [&](int32_t base, const int32_t (&from)[4], uint32_t buf) {
+  const auto load_k = [&](int32_t t, const Pages& from, uint32_t buf) {
+#pragma unroll
     for (int i = 0; i < NK; ++i) {
       const uint32_t at = (wave * NK + i) * 64u, c = at + lane, row = c / CH;
-      const uint32_t key = swap23(row), part = (c % CH) ^ (row & MASK);
-      const T* src = (const T*)a.k + (size_t)pick(from, key >> 4) * per_page + head +
-                     (((uint32_t)base + key) & in_page) * D + 8 * part;
-      to_lds(src, &kt[buf][at]);
-    }
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t at = (wave * NV + i) * 64u, c = at + lane, d = c >> 3;
-      const uint32_t part = (c & 7u) ^ (d & 7u);
-      const T* src = (const T*)a.v + (size_t)pick(from, part >> 1) * per_page + head + (size_t)d * a.page +
-                     (((uint32_t)base + 8 * part) & in_page);
-      to_lds(src, &vt[buf][at]);
+      const uint32_t key = swap23(row), part = (c % CH) ^ spread<CH>(row);
+      to_lds((const T*)a.k + (size_t)pick(from, key >> 4) * per_page + head +
+                 (((uint32_t)(start + 64 * t) + key) & in_page) * D + 8 * part, &kt[buf][at]);
     }
   };
-  int32_t next_pg[4] = {-1, -1, -1, -1};
-  if (start < end) {
-    pages_of(start, pg);
-    load(start, pg, 0);
-    pages_of(start + (int32_t)kManyKeys, next_pg);
-  }
-  uint32_t buf = 0;
-  for (int32_t base = start; base < end; base += (int32_t)kManyKeys, buf ^= 1u) {
+  const auto load_v = [&](int32_t t, const Pages& from, uint32_t buf) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t at = (wave * NV + i) * 64u, c = at + lane, d = c >> 3;
+      const uint32_t part = (c & 7u) ^ spread<8>(d);
+      to_lds((const T*)a.v + (size_t)pick(from, part >> 1) * per_page + head + (size_t)d * a.page +
+                 (((uint32_t)(start + 64 * t) + 8 * part) & in_page), &vt[buf][at]);
+    }
+  };
+  const auto landed = [&] {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    int32_t after[4];
-    if (base + (int32_t)kManyKeys < end) {
-      load(base + (int32_t)kManyKeys, next_pg, buf ^ 1u);
-      pages_of(base + 2 * (int32_t)kManyKeys, after);
-    } else {
-      for (int i = 0; i < 4; ++i) after[i] = -1;
+  };
+  uint32_t k_at[KS], v_at[4];  // the lane's pieces of rows r32
+#pragma unroll
+  for (int k = 0; k < KS; ++k) k_at[k] = r32 * CH + ((2 * k + half) ^ spread<CH>(r32));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v_at[k] = r32 * 8 + ((2 * k + half) ^ spread<8>(r32));
+
+  v8 pend[2];  // the rounded p of the group before, whose second product is still to come
+  pend[0] = pend[1] = (v8)(T)0.0f;
+  f32x16 sc = (f32x16)0.0f;
+
+  // One group of 32 entries, c = 0 or 1 of tile t, its scores in sc.  `vb` and `kb`: the buffers of the group
+  // before's values (its pieces from 2 (1 - c) on) and of the group behind's keys.
+  const auto group = [&](auto c_, int32_t t, const Pages& pages, const v8* vb,
+                         const v8* kb) __attribute__((always_inline)) {
+    constexpr int c = decltype(c_)::value;
+    const int32_t base = start + 64 * t + 32 * c;
+    const bool there = (c ? pages.x[2] | pages.x[3] : pages.x[0] | pages.x[1]) >= 0;
+    if (!there || base + 32 > seen_by_all)
+      // register i of the lane is entry 16 (i / 8) + 8 half + i % 8 of the group
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (pages.x[2 * c + (i >> 3)] < 0 || base + 16 * (i >> 3) + 8 * (int32_t)half + (i & 7) >= limit)
+          sc[i] = -kInf;
+    float top = sc[0];
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+    top *= scale;
+    float f = 1.0f;
+    const bool moved = __builtin_amdgcn_ballot_w64(top > m + kSlack) != 0ull;
+    if (moved) {
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float next = fmaxf(m, top);
+      f = exp2_fast(m - or_zero(next));
+      m = next;
+      l *= f;
     }
-    const bool there = (pg[0] | pg[1] | pg[2] | pg[3]) >= 0;
-    if (!there || base + (int32_t)kManyKeys > q.len) {  // what is not an entry may hold anything
-      for (uint32_t c = tid; c < D * 8u; c += kBlock) {
-        const uint32_t part = (c & 7u) ^ ((c >> 3) & 7u);
-        const int32_t run = part & 4u ? (part & 2u ? pg[3] : pg[2]) : (part & 2u ? pg[1] : pg[0]);
-        v8 x = vt[buf][c];
-        for (int i = 0; i < 8; ++i)
-          if (run < 0 || base + (int32_t)(8 * part) + i >= q.len) x[i] = (T)0.0f;
-        vt[buf][c] = x;
+    const float sub = -or_zero(m);
+    v8 pf[2];
+    f32x16 behind = (f32x16)0.0f;
+    float l0 = 0.0f, l1 = 0.0f;
+    constexpr int STEPS = KS > 2 * DT ? KS : 2 * DT;
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+      if (u < 2 * DT) o[u % DT] = M::mma32(vb[v_at[2 * (1 - c) + u / DT] + (u % DT) * 32 * 8], pend[u / DT], o[u % DT]);
+      if (u < KS) behind = M::mma32(kb[k_at[u]], qf[u], behind);
+#pragma unroll
+      for (int x = u * 16 / STEPS; x < (u + 1) * 16 / STEPS; ++x) {
+        const float e = exp2_fast(fmaf(sc[x], scale, sub));
+        if (x & 1) l1 += e; else l0 += e;
+        pf[x >> 3][x & 7] = (T)e;  // rounded for the second product only, as above
+      }
+    }
+    // Put the exponentials between the products (left alone, they sink behind the next branch): the
+    // operands' reads run ahead by four, then a product, a read and an element in turn.
+    l0 += l1;
+    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l0));
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int u = 0; u < KS + 2 * DT; ++u) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+    }
+    l += l0;
+    if (moved)
+#pragma unroll
+      for (int t2 = 0; t2 < DT; ++t2) o[t2] *= f;
+    pend[0] = pf[0];
+    pend[1] = pf[1];
+    sc = behind;
+  };
+  const std::integral_constant<int, 0> c0;
+  const std::integral_constant<int, 1> c1;
+
+  Pages now = pages_of(0), next = pages_of(1), then = pages_of(2);
+  if (tiles) {
+    load_k(0, now, 0);
+    load_v(0, now, 0);
+    if (tiles > 1) load_k(1, next, 1);
+    // the first group has no group before: zeros times zero
+    for (uint32_t i = tid; i < D * 8u; i += kBlock) vt[1][i] = (v8)(T)0.0f;
+    landed();
+#pragma unroll
+    for (int k = 0; k < KS; ++k) sc = M::mma32(kt[0][k_at[k]], qf[k], sc);
+  }
+  // Tile t: its first group while V of tile t - 1 and K of tile t are there; then everybody is done with
+  // both, and V of tile t + 1 and K of tile t + 2 take their places.
+  const auto body = [&](auto buf_, int32_t t) __attribute__((always_inline)) {
+    constexpr uint32_t buf = decltype(buf_)::value;
+    if (t < wave_tiles) group(c0, t, now, vt[buf ^ 1u], kt[buf] + 32 * CH);
+    landed();
+    if (t + 1 < tiles) load_v(t + 1, next, buf ^ 1u);
+    if (t + 2 < tiles) load_k(t + 2, then, buf);
+    const int32_t base = start + 64 * t;
+    if ((now.x[0] | now.x[1] | now.x[2] | now.x[3]) < 0 || base + 64 > q.len) {
+      for (uint32_t i = tid; i < D * 8u; i += kBlock) {  // what is not an entry may hold anything
+        const uint32_t part = (i & 7u) ^ spread<8>(i >> 3);
+        const int32_t run = part & 4u ? (part & 2u ? now.x[3] : now.x[2]) : (part & 2u ? now.x[1] : now.x[0]);
+        v8 x = vt[buf][i];
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (run < 0 || base + (int32_t)(8 * part) + y >= q.len) x[y] = (T)0.0f;
+        vt[buf][i] = x;
       }
       __syncthreads();
     }
-    if (base < wave_end) {
-      float z[32];
-      for (int b = 0; b < 2; ++b) {
-        f32x16 sc = (f32x16)0.0f;
-        const uint32_t row = 32u * b + r32;
-        for (int k = 0; k < KS; ++k) sc = M::mma32(kt[buf][row * CH + ((2 * k + half) ^ (row & MASK))], qf[k], sc);
-        for (int i = 0; i < 16; ++i) z[16 * b + i] = sc[i] * p.scale2;
-      }
-      // register i of the lane is entry 16 (i / 8) + 8 half + i % 8 of the tile
-      if (!there || base + (int32_t)kManyKeys > seen_by_all)
-        for (int i = 0; i < 32; ++i) {
-          const int32_t e = base + 16 * (i >> 3) + 8 * (int32_t)half + (i & 7);
-          if (pg[i >> 3] < 0 || e >= limit) z[i] = -kInf;
-        }
-      float top = z[0];
-      for (int i = 1; i < 32; ++i) top = fmaxf(top, z[i]);
-      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(m, top);
-        const float f = exp2_fast(m - or_zero(next));
-        m = next;
-        l *= f;
-        for (int t = 0; t < DT; ++t) o[t] *= f;
-      }
-      const float sub = or_zero(m);
-      v8 pf[4];
-      for (int i = 0; i < 32; ++i) {
-        const float e = exp2_fast(z[i] - sub);
-        l += e;
-        pf[i >> 3][i & 7] = (T)e;  // rounded for the second product only, as above
-      }
-      for (int t = 0; t < DT; ++t) {
-        const uint32_t d = 32u * t + r32;
-        for (int k = 0; k < 4; ++k) o[t] = M::mma32(vt[buf][d * 8 + ((2 * k + half) ^ (d & 7u))], pf[k], o[t]);
-      }
+    if (t < wave_tiles) {
+      group(c1, t, now, vt[buf], kt[buf ^ 1u]);
+      if (t + 1 == wave_tiles)
+#pragma unroll
+        for (int u = 0; u < 2 * DT; ++u)
+          o[u % DT] = M::mma32(vt[buf][v_at[2 + u / DT] + (u % DT) * 32 * 8], pend[u / DT], o[u % DT]);
     }
-    for (int i = 0; i < 4; ++i) {
-      pg[i] = next_pg[i];
-      next_pg[i] = after[i];
-    }
+    now = next;
+    next = then;
+    then = pages_of(t + 3);
+  };
+  for (int32_t t = 0; t < tiles; t += 2) {
+    body(std::integral_constant<uint32_t, 0>{}, t);
+    if (t + 1 < tiles) body(std::integral_constant<uint32_t, 1>{}, t + 1);
   }
   l += __shfl_xor(l, 32);
   if (!is) return;
   const size_t part = part_row(p, split, s, h) + r;
   if (p.n_split > 1) {
     if (half == 0) p.part_ml[part] = make_float2(m, l);
+#pragma unroll
     for (int t = 0; t < DT; ++t)
+#pragma unroll
       for (int c = 0; c < 4; ++c)
         *(f32x4*)(p.part_o + part * D + 32 * t + 8 * c + 4 * half) =
             f32x4{o[t][4 * c], o[t][4 * c + 1], o[t][4 * c + 2], o[t][4 * c + 3]};
@@ -526,7 +662,9 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
   }
   const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
   const size_t row = (size_t)(q.t0 + (int32_t)j) * a.n_q + h * a.group + g;
+#pragma unroll
   for (int t = 0; t < DT; ++t)
+#pragma unroll
     for (int c = 0; c < 4; ++c) {
       const float x[4] = {o[t][4 * c] * inv, o[t][4 * c + 1] * inv, o[t][4 * c + 2] * inv, o[t][4 * c + 3] * inv};
       store4<M>((T*)p.out + row * D + 32 * t + 8 * c + 4 * half, x);
@@ -534,71 +672,131 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
   if (p.lse && half == 0) p.lse[row] = l == 0.0f ? -kInf : (m + log2f(l)) * kLn2;
 }
 
-// weight = decay * weight + the sum of p over a sequence's rows, which another product of the keys
-// with the queries gives, the entries in the lanes now and the rows in their registers: 32 entries a
-// wavefront with their keys in registers, 32 rows at a time from LDS.
+// weight = decay * weight + the sum of p over a sequence's rows, which another product of the keys with
+// the queries gives, the entries in the lanes now and the rows in their registers: 64 entries a wavefront
+// with their keys in registers, 64 rows at a time from double-buffered LDS.  Bound by the exponentials.
+constexpr uint32_t kWeightKeys = 256, kWeightRows = 64;
+
 template <typename M, int D>
-__global__ __launch_bounds__(kBlock) void kv_weight_many_kernel(Attn p, float decay) {
+__global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kernel(Attn p, float decay) {
   typedef typename M::t T;
   typedef typename M::v8 v8;
-  constexpr uint32_t CH = D / 8, MASK = CH - 1 < 15 ? CH - 1 : 15;
-  constexpr int KS = D / 16;
-  __shared__ v8 qt[32 * CH];
-  __shared__ float base[32];
-  __shared__ int32_t lim[32];
+  constexpr uint32_t CH = D / 8;
+  constexpr int KS = D / 16, NQ = CH / 4;
+  __shared__ v8 qt[2][kWeightRows * CH];
+  __shared__ f32x4 base[2][kWeightRows / 4];  // minus the rows' log sums, in powers of two
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 63u, half = lane >> 5, c32 = lane & 31u;
+  const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
   const KvSeq q = kv_seq(a, s);
   const uint32_t rows = (uint32_t)q.n * a.group;
-  const int32_t first = (int32_t)(blockIdx.x * (kBlock / 2));
+  const int32_t first = (int32_t)(spread_piece(blockIdx.x, gridDim.x) * kWeightKeys), mine = first + (int32_t)(64u * wave);
   if (rows == 0 || first >= q.len) return;
-  const int32_t e = first + (int32_t)(32u * (tid >> 6) + c32), old = q.len - q.n;
-  const int32_t page = e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
-  const uint32_t slot = (uint32_t)e & (a.page - 1u);
-  const T* key = (const T*)a.k + kv_base(a, page < 0 ? 0 : page, h) + (size_t)slot * D;
-  v8 kf[KS];
-  for (int k = 0; k < KS; ++k) kf[k] = *(const v8*)(key + 16 * k + 8 * half);
-  float sum = 0.0f;
-  // rows of tokens before entry `first` see nothing here
-  const uint32_t from = first > old ? ((uint32_t)(first - old) * a.group) & ~31u : 0u;
-  for (uint32_t r0 = from; r0 < rows; r0 += 32u) {
-    for (uint32_t c = tid; c < 32u * CH; c += kBlock) {
-      const uint32_t row = c / CH, part = c % CH, r = r0 + row;
-      v8 x = (v8)(T)0.0f;
-      if (r < rows)
-        x = *(const v8*)((const T*)p.q.p + (size_t)(q.t0 + (int32_t)(r / a.group)) * p.q.tok +
-                         (h * a.group + r % a.group) * p.q.head + 8 * part);
-      qt[row * CH + (part ^ (row & MASK))] = x;
-    }
-    if (tid < 32u) {
-      const uint32_t r = r0 + tid;
-      float b = kInf;
-      int32_t to = 0;
-      if (r < rows) {
-        const int32_t j = (int32_t)(r / a.group);
-        b = p.lse[(size_t)(q.t0 + j) * a.n_q + h * a.group + r % a.group] * kLog2e;
-        if (b == -kInf) b = kInf;
-        to = old + j + 1;
-      }
-      base[tid] = b;
-      lim[tid] = to;
-    }
-    __syncthreads();
-    f32x16 sc = (f32x16)0.0f;
-    for (int k = 0; k < KS; ++k) sc = M::mma32(qt[c32 * CH + ((2 * k + half) ^ (c32 & MASK))], kf[k], sc);
-    float part = 0.0f;  // a tile's sum first: thousands of rows added one by one would lose bits
-    for (int i = 0; i < 16; ++i) {
-      const uint32_t row = 8u * (i >> 2) + 4u * half + (i & 3);
-      const float x = exp2_fast(sc[i] * p.scale2 - base[row]);
-      part += e < lim[row] ? x : 0.0f;
-    }
-    sum += part;
-    __syncthreads();
+  const int32_t old = q.len - q.n;
+  const float scale = magnitude(p.scale2);
+  const bool negate = p.scale2 < 0.0f;
+  v8 kf[2][KS];
+  int32_t page[2];
+  for (int y = 0; y < 2; ++y) {
+    const int32_t e = mine + 32 * y + (int32_t)c32;
+    page[y] = e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
+    const T* key = (const T*)a.k + kv_base(a, page[y] < 0 ? 0 : page[y], h) + (size_t)((uint32_t)e & (a.page - 1u)) * D;
+    for (int k = 0; k < KS; ++k) kf[y][k] = signed_row(*(const v8*)(key + 16 * k + 8 * half), negate);
   }
-  sum += __shfl_xor(sum, 32);
-  if (page < 0 || half) return;
-  float* w = a.weight + kv_word(a, page, h) + slot;
-  *w = fmaf(decay, *w, sum);
+  // rows of tokens before entry `first` see nothing here
+  const uint32_t from = first > old ? ((uint32_t)(first - old) * a.group) & ~(kWeightRows - 1u) : 0u;
+  const int32_t tiles = from < rows ? (int32_t)((rows - from + kWeightRows - 1u) / kWeightRows) : 0;
+  // token and head of the lane's rows of the next tile, moved on without dividing
+  const uint32_t dj = kWeightRows / a.group, dg = kWeightRows % a.group;
+  uint32_t rj[NQ], rg[NQ], bj = 0, bg = 0;
+  for (int i = 0; i < NQ; ++i) {
+    const uint32_t r = from + ((wave * NQ + i) * 64u + lane) / CH;
+    rj[i] = r / a.group;
+    rg[i] = r % a.group;
+  }
+  if (tid < kWeightRows) {
+    bj = (from + tid) / a.group;
+    bg = (from + tid) % a.group;
+  }
+  const auto on = [&](uint32_t& j, uint32_t& g) {
+    j += dj;
+    g += dg;
+    if (g >= a.group) {
+      g -= a.group;
+      ++j;
+    }
+  };
+  const auto load = [&](uint32_t buf) {
+    for (int i = 0; i < NQ; ++i) {
+      const uint32_t at = (wave * NQ + i) * 64u, c = at + lane, row = c / CH, part = (c % CH) ^ spread<CH>(row);
+      const uint32_t j = rj[i] < (uint32_t)q.n ? rj[i] : (uint32_t)q.n - 1u;  // a row behind the last counts nothing
+      to_lds((const T*)p.q.p + (size_t)(q.t0 + (int32_t)j) * p.q.tok + (h * a.group + rg[i]) * p.q.head + 8 * part,
+             &qt[buf][at]);
+      on(rj[i], rg[i]);
+    }
+  };
+  float b = 0.0f;
+  const auto load_base = [&] {
+    if (tid < kWeightRows) {
+      b = bj < (uint32_t)q.n ? p.lse[(size_t)(q.t0 + (int32_t)bj) * a.n_q + h * a.group + bg] : kInf;
+      on(bj, bg);
+    }
+  };
+  const auto put_base = [&](uint32_t buf) {  // a row that sees nothing has -inf
+    if (tid < kWeightRows) ((float*)base[buf])[tid] = b == -kInf ? -kInf : b * -kLog2e;
+  };
+  float sum[2] = {0.0f, 0.0f};
+  if (tiles) {
+    load(0);
+    load_base();
+  }
+  for (int32_t t = 0; t < tiles; ++t) {
+    const uint32_t buf = (uint32_t)t & 1u, r0 = from + (uint32_t)t * kWeightRows;
+    put_base(buf);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < tiles) {
+      load(buf ^ 1u);
+      load_base();
+    }
+    const uint32_t last = r0 + kWeightRows - 1u < rows ? r0 + kWeightRows - 1u : rows - 1u;
+    if (old + (int32_t)(last / a.group) + 1 <= mine) continue;  // its rows see none of the wavefront's entries
+    const bool whole = old + (int32_t)(r0 / a.group) + 1 >= mine + 64;
+    for (uint32_t x = 0; x < 2; ++x) {
+      f32x16 sc[2];
+      sc[0] = sc[1] = (f32x16)0.0f;
+      for (int k = 0; k < KS; ++k) {
+        const uint32_t row = 32u * x + c32;
+        const v8 f = qt[buf][row * CH + ((2 * k + half) ^ spread<CH>(row))];
+        sc[0] = M::mma32(f, kf[0][k], sc[0]);
+        sc[1] = M::mma32(f, kf[1][k], sc[1]);
+      }
+      f32x4 n[4];  // register i is row 8 (i / 4) + 4 half + i % 4 of the 32
+      for (uint32_t i = 0; i < 4; ++i) n[i] = base[buf][8 * x + 2 * i + half];
+      for (int y = 0; y < 2; ++y) {
+        float part = 0.0f;  // a tile's sum first: thousands of rows added one by one would lose bits
+        if (whole) {
+          for (int i = 0; i < 16; ++i) part += exp2_fast(fmaf(sc[y][i], scale, n[i >> 2][i & 3]));
+        } else {
+          const int32_t e = mine + 32 * y + (int32_t)c32;
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t r = r0 + 32u * x + 8u * (i >> 2) + 4u * half + (i & 3);
+            // entry e is seen from row (e - old) * group on
+            const bool sees = (int64_t)r >= (int64_t)(e - old) * (int64_t)a.group;
+            const float v = exp2_fast(fmaf(sc[y][i], scale, n[i >> 2][i & 3]));
+            part += sees ? v : 0.0f;
+          }
+        }
+        sum[y] += part;
+      }
+    }
+  }
+  for (int y = 0; y < 2; ++y) {
+    sum[y] += __shfl_xor(sum[y], 32);
+    if (page[y] < 0 || half) continue;
+    float* w = a.weight + kv_word(a, page[y], h) + ((uint32_t)(mine + 32 * y + (int32_t)c32) & (a.page - 1u));
+    *w = fmaf(decay, *w, sum[y]);
+  }
 }
 
 // ------------------------------------------------------------------ plans
@@ -613,17 +811,17 @@ struct Plan {
   size_t o, ml, many_o, many_ml, scores, lse, keys, bytes;
 };
 
-constexpr uint64_t kBlocksWanted = 2048;  // eight blocks a compute unit: enough loads in flight
+constexpr uint64_t kBlocksWanted = 4096;  // 16 a compute unit: enough loads in flight, and even ends
 
-// The entries of a split: at least 256, few enough that `units` of them give the blocks wanted, at
-// most what LDS has page ids for, whole pages and whole rounds of the block's tiles.
+// The entries of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
+// most what LDS has page ids for, whole pages and whole rounds of the block's wavefronts.
 uint32_t chunk_of(const KvArgs& a, uint64_t entries, uint64_t units, uint64_t wanted, uint32_t least) {
   const uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
   uint64_t c = (entries + splits - 1) / splits;
   c = c < least ? least : c;
   const uint64_t most = (uint64_t)kPagesLds * a.page;
   c = c > most ? most : c;
-  return (uint32_t)up(c, a.page > 128 ? a.page : 128);
+  return (uint32_t)up(c, 256);
 }
 
 Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
@@ -666,7 +864,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.many_ml = take((size_t)p.many_split * pairs * row_most * sizeof(float2));
   }
   if (weights && !p.many) {
-    p.score_len = (uint32_t)up(a.max_len, 32);
+    p.score_len = (uint32_t)up(a.max_len, 64);
     p.scores = take(pairs * p.few_cap * p.score_len * sizeof(float));
   }
   if (weights && p.many) p.lse = take((size_t)a.n_tok * a.n_q * sizeof(float));
@@ -730,7 +928,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.rows_to = row_most;
     launch(kv_many_kernel<M, D>, dim3(a.n_kv * plan.many_split, (row_most + kManyRows - 1) / kManyRows, a.n_seq));
     if (plan.many_split > 1) join(row_most);
-    if (weights) launch(kv_weight_many_kernel<M, D>, dim3((a.max_len + kBlock / 2 - 1) / (kBlock / 2), a.n_kv, a.n_seq),
+    if (weights) launch(kv_weight_many_kernel<M, D>, dim3((a.max_len + kWeightKeys - 1) / kWeightKeys, a.n_kv, a.n_seq),
                         decay);
   }
   return hipGetLastError();

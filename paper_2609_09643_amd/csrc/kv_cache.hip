@@ -639,7 +639,7 @@ __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, u
   __shared__ float lds[kBlock / 64];
   const uint32_t h = blockIdx.y, tid = threadIdx.x, lane = tid & 63u;
   const uint32_t chunks = (a.max_len + a.page * kScorePages - 1) / (a.page * kScorePages);
-  const uint32_t j = blockIdx.x / chunks, base = (blockIdx.x % chunks) * kScorePages;
+  const uint32_t j = blockIdx.x / chunks, base = spread_piece(blockIdx.x % chunks, chunks) * kScorePages;
   const KvSeq q = kv_seq(a, blockIdx.z);
   if ((int32_t)j >= q.n) return;
   const size_t t = (size_t)q.t0 + j;
