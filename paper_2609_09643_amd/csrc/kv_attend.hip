@@ -51,7 +51,12 @@ constexpr uint32_t kBlock = 256;
 constexpr uint32_t kWaves = kBlock / 64;
 constexpr uint32_t kRowsFew = 32;         // rows of a (sequence, kv head) up to which the few-rows kernel serves it
 constexpr uint32_t kPagesLds = 1024;      // page ids of one block's entries
-constexpr uint32_t kManyRows = 128, kManyKeys = 64;
+constexpr uint32_t kPagesPast = 64;       // and, of no pages, those of tiles read ahead
+constexpr uint32_t kManyKeys = 64;
+// The many-rows kernel: wavefronts of a block, 32 rows each, and tiles of 64 entries in LDS.
+constexpr uint32_t many_waves(uint32_t dim) { return dim <= 128 ? 8 : 4; }
+constexpr uint32_t many_rows(uint32_t dim) { return 32 * many_waves(dim); }
+
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -406,6 +411,9 @@ __device__ __forceinline__ void to_lds(const void* from, void* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// Waits for the wavefront's loads, those into LDS among them (vmcnt(0)).
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
 // The order in which rows of a left operand hold entries: bits 2 and 3 change places.
 __device__ __forceinline__ uint32_t swap23(uint32_t x) {
   return (x & ~12u) | ((x & 4u) << 1) | ((x & 8u) >> 1);
@@ -418,6 +426,21 @@ __device__ __forceinline__ uint32_t spread(uint32_t row) {
   return CH == 8 ? (row >> 1) & 7u : row & 15u;
 }
 
+// The same for rows that keep only the offsets' lane-dependent part small: a kibibyte (64 pieces, what a
+// wavefront loads at once) takes kRun bytes, the 64 more bytes turning the next one's banks by a quarter, and
+// inside it a row's pieces are xored with two bits of the row.  16 rows' pieces c lie in different banks, and the
+// address of piece c is the lane's for c mod 4 and a constant.
+constexpr uint32_t kRun = 1024 + 64;
+template <uint32_t CH>
+__device__ __forceinline__ uint32_t turn(uint32_t row) {
+  return CH == 8 ? (row >> 1) & 3u : CH == 16 ? row & 3u : (row & 1u) | ((row >> 2) & 2u);
+}
+template <uint32_t CH>
+__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t c) {
+  const uint32_t at = row * CH;  // in pieces
+  return at / 64u * kRun + at % 64u * 16u + (c ^ turn<CH>(row)) * 16u;
+}
+
 // A row of the queries, negated where the scale is negative: the kernels below scale by its magnitude.
 template <typename v8>
 __device__ __forceinline__ v8 signed_row(v8 x, bool negate) {
@@ -428,19 +451,22 @@ __device__ __forceinline__ v8 signed_row(v8 x, bool negate) {
 // A scale of 0 would make NaN of the scores that a mask sets to -inf.
 __device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(scale2), 1e-35f); }
 
-// Attention of 128 rows over a chunk of entries, 32 rows a wavefront, 64 entries at a time from
+// Attention of 128 or 256 rows over a chunk of entries, 32 rows a wavefront, 64 entries at a time from
 // double-buffered LDS: a turn's new tokens over their session.  Bound by the matrix cores and, nearly as
 // much, by the exponentials (a quarter of the rate) and the additions and roundings beside them, so the
 // two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
 // the second product of the group before and the first product of the group behind.
 template <typename M, int D>
-__global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {
+__global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {
   typedef typename M::t T;
   typedef typename M::v8 v8;
   constexpr uint32_t CH = D / 8;
-  constexpr int KS = D / 16, DT = D / 32, NK = CH / 4, NV = D / 32;
-  __shared__ v8 kt[2][kManyKeys * CH];
-  __shared__ v8 vt[2][D * 8];
+  constexpr uint32_t WAVES = many_waves(D), ROWS = many_rows(D);
+  constexpr int KS = D / 16, DT = D / 32, NK = CH / WAVES, NV = D / 8 / WAVES;
+  // an array for each buffer: the compiler waits for every load into an array before it reads the array
+  constexpr uint32_t KB = kManyKeys * D * 2 / 1024 * kRun, VB = D * 128 / 1024 * kRun;
+  __shared__ alignas(16) char kt0[KB], kt1[KB], vt0[VB], vt1[VB];
+  __shared__ int32_t pg[kPagesLds + kPagesPast];
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.x % a.n_kv, split = blockIdx.x / a.n_kv, s = blockIdx.z, tid = threadIdx.x;
   const uint32_t lane = tid & 63u, half = lane >> 5, r32 = lane & 31u;
@@ -448,16 +474,16 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
   const KvSeq q = kv_seq(a, s);
   const uint32_t rows = (uint32_t)q.n * a.group;
   const uint32_t tile = gridDim.y - 1u - blockIdx.y;  // the longest first
-  if (rows <= p.rows_from || tile * kManyRows >= rows) return;
+  if (rows <= p.rows_from || tile * ROWS >= rows) return;
   const int32_t old = q.len - q.n;
-  const uint32_t r = tile * kManyRows + 32u * wave + r32;
+  const uint32_t r = tile * ROWS + 32u * wave + r32;
   const bool is = r < rows;
   const uint32_t j = (is ? r : 0u) / a.group, g = (is ? r : 0u) % a.group;
   const int32_t limit = is ? old + (int32_t)j + 1 : 0;
   // entries that some row of the block (of the wavefront) sees, and that all rows of the wavefront see
   const auto token = [&](uint32_t x) { return (int32_t)((x < rows ? x : rows - 1u) / a.group); };
-  const int32_t block_end = old + token((tile + 1u) * kManyRows - 1u) + 1;
-  const uint32_t w0 = tile * kManyRows + 32u * wave;
+  const int32_t block_end = old + token((tile + 1u) * ROWS - 1u) + 1;
+  const uint32_t w0 = tile * ROWS + 32u * wave;
   const int32_t start = (int32_t)(split * p.chunk);
   if (start >= q.len && split) return;
   int32_t end = block_end < q.len ? block_end : q.len;
@@ -486,16 +512,31 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
 
   const size_t head = (size_t)h * a.page * D, per_page = (size_t)a.n_kv * a.page * D;
   const uint32_t in_page = a.page - 1u;
-  struct Pages {  // of a tile's four runs of 16 entries
+  const bool wide = a.page >= kManyKeys;
+  // The page ids of the block's entries; a tile's are read a tile ahead of their use.
+  const uint32_t n_ids = end > start ? (uint32_t)(end - start + (int32_t)in_page) >> a.page_bits : 0u;
+  for (uint32_t i = tid; i < n_ids + kPagesPast; i += 64u * WAVES)
+    pg[i] = i < n_ids ? kv_page(a, q, (int32_t)(((uint32_t)start >> a.page_bits) + i)) : -1;
+  __syncthreads();
+  struct Pages {  // of a tile's four runs of 16 entries, x[0] of all where a page holds the tile
     int32_t x[4];
   };
-  const auto pages_of = [&](int32_t t) {
+  const auto ids_of = [&](int32_t t) __attribute__((always_inline)) {
     Pages to;
+    to.x[0] = pg[(uint32_t)(64 * t) >> a.page_bits];
+    to.x[1] = to.x[2] = to.x[3] = to.x[0];
+    if (!wide)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int32_t e = start + 64 * t + 16 * i;
-      to.x[i] = t < tiles && e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
-    }
+      for (int i = 1; i < 4; ++i) to.x[i] = pg[(uint32_t)(64 * t + 16 * i) >> a.page_bits];
+    return to;
+  };
+  const auto uniform = [&](const Pages& from) __attribute__((always_inline)) {
+    Pages to;
+    to.x[0] = __builtin_amdgcn_readfirstlane(from.x[0]);
+    to.x[1] = to.x[2] = to.x[3] = to.x[0];
+    if (!wide)
+#pragma unroll
+      for (int i = 1; i < 4; ++i) to.x[i] = __builtin_amdgcn_readfirstlane(from.x[i]);
     return to;
   };
   const auto pick = [&](const Pages& from, uint32_t i) {
@@ -503,42 +544,77 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
     const int32_t z = i & 2u ? y : x;
     return z < 0 ? 0 : z;
   };
-  const auto load_k = [&](int32_t t, const Pages& from, uint32_t buf) {
+  // Where a lane's pieces of a tile lie in a page of 64 entries or more, which holds the whole tile: the rest
+  // of their address is the same for all lanes.
+  uint32_t k_off[NK], v_off[NV];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) {
+    const uint32_t c = (wave * NK + i) * 64u + lane, row = c / CH;
+    k_off[i] = (swap23(row) * D + 8 * ((c % CH) ^ turn<CH>(row))) * 2u;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const uint32_t c = (wave * NV + i) * 64u + lane, d = c >> 3;
+    v_off[i] = (d * a.page + 8 * ((c & 7u) ^ turn<8>(d))) * 2u;
+  }
+  const auto load_k = [&](int32_t t, const Pages& from, char* kt) __attribute__((always_inline)) {
+    const uint32_t e = (uint32_t)(start + 64 * t);
+    if (wide) {
+      const char* at = (const char*)((const T*)a.k + (size_t)pick(from, 0) * per_page + head + (e & in_page) * D);
+#pragma unroll
+      for (int i = 0; i < NK; ++i) to_lds(at + k_off[i], kt + (wave * NK + i) * kRun);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const uint32_t at = (wave * NK + i) * 64u, c = at + lane, row = c / CH;
-      const uint32_t key = swap23(row), part = (c % CH) ^ spread<CH>(row);
-      to_lds((const T*)a.k + (size_t)pick(from, key >> 4) * per_page + head +
-                 (((uint32_t)(start + 64 * t) + key) & in_page) * D + 8 * part, &kt[buf][at]);
+      const uint32_t key = swap23(row), part = (c % CH) ^ turn<CH>(row);
+      to_lds((const T*)a.k + (size_t)pick(from, key >> 4) * per_page + head + ((e + key) & in_page) * D + 8 * part,
+             kt + at / 64u * kRun);
     }
   };
-  const auto load_v = [&](int32_t t, const Pages& from, uint32_t buf) {
+  const auto load_v = [&](int32_t t, const Pages& from, char* vt) __attribute__((always_inline)) {
+    const uint32_t e = (uint32_t)(start + 64 * t);
+    if (wide) {
+      const char* at = (const char*)((const T*)a.v + (size_t)pick(from, 0) * per_page + head + (e & in_page));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) to_lds(at + v_off[i], vt + (wave * NV + i) * kRun);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const uint32_t at = (wave * NV + i) * 64u, c = at + lane, d = c >> 3;
-      const uint32_t part = (c & 7u) ^ spread<8>(d);
+      const uint32_t part = (c & 7u) ^ turn<8>(d);
       to_lds((const T*)a.v + (size_t)pick(from, part >> 1) * per_page + head + (size_t)d * a.page +
-                 (((uint32_t)(start + 64 * t) + 8 * part) & in_page), &vt[buf][at]);
+                 ((e + 8 * part) & in_page), vt + at / 64u * kRun);
     }
   };
   const auto landed = [&] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_loads();
     __syncthreads();
   };
-  uint32_t k_at[KS], v_at[4];  // the lane's pieces of rows r32
+  // the lane's pieces of rows r32, by their number's second bit: the rest of the number is a constant offset
+  uint32_t k_at[2], v_at[2];
 #pragma unroll
-  for (int k = 0; k < KS; ++k) k_at[k] = r32 * CH + ((2 * k + half) ^ spread<CH>(r32));
-#pragma unroll
-  for (int k = 0; k < 4; ++k) v_at[k] = r32 * 8 + ((2 * k + half) ^ spread<8>(r32));
+  for (uint32_t k = 0; k < 2; ++k) {
+    k_at[k] = piece_at<CH>(r32, 2 * k + half);
+    v_at[k] = piece_at<8>(r32, 2 * k + half);
+  }
+  const auto k_piece = [&](const char* kb, int k, uint32_t group) __attribute__((always_inline)) {
+    return *(const v8*)(kb + k_at[k & 1] + (k >> 1) * 64 + group * (32 * CH / 64) * kRun);
+  };
+  const auto v_piece = [&](const char* vb, int k, int dims) __attribute__((always_inline)) {
+    return *(const v8*)(vb + v_at[k & 1] + (k >> 1) * 64 + dims * 4 * kRun);
+  };
 
   v8 pend[2];  // the rounded p of the group before, whose second product is still to come
   pend[0] = pend[1] = (v8)(T)0.0f;
   f32x16 sc = (f32x16)0.0f;
 
   // One group of 32 entries, c = 0 or 1 of tile t, its scores in sc.  `vb` and `kb`: the buffers of the group
-  // before's values (its pieces from 2 (1 - c) on) and of the group behind's keys.
-  const auto group = [&](auto c_, int32_t t, const Pages& pages, const v8* vb,
-                         const v8* kb) __attribute__((always_inline)) {
+  // before's values (its pieces from 2 (1 - c) on) and of the group behind's keys (its rows from 32 (1 - c) on).
+  const auto group = [&](auto c_, int32_t t, const Pages& pages, const char* vb,
+                         const char* kb) __attribute__((always_inline)) {
     constexpr int c = decltype(c_)::value;
     const int32_t base = start + 64 * t + 32 * c;
     const bool there = (c ? pages.x[2] | pages.x[3] : pages.x[0] | pages.x[1]) >= 0;
@@ -561,34 +637,40 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
       l *= f;
     }
     const float sub = -or_zero(m);
-    v8 pf[2];
+    // A product, a later product's read and an element in turn.  The order is held as written: left alone, the
+    // exponentials sink behind the next branch and each read goes next to its product.
+    static_assert(KS == 2 * DT, "as many products of each kind");
+    constexpr int N = 2 * KS, AHEAD = 6;
+    v8 pf[2], f_[N];
     f32x16 behind = (f32x16)0.0f;
-    float l0 = 0.0f, l1 = 0.0f;
-    constexpr int STEPS = KS > 2 * DT ? KS : 2 * DT;
+    float e_[16], l0 = 0.0f, l1 = 0.0f;
+    const auto read = [&](int u) __attribute__((always_inline)) {
+      const int i = u >> 1;
+      f_[u] = u & 1 ? k_piece(kb, i, 1 - c) : v_piece(vb, 2 * (1 - c) + i / DT, i % DT);
+    };
+    const auto rest = [&](int x) __attribute__((always_inline)) {
+      if (x & 1) l1 += e_[x]; else l0 += e_[x];
+      pf[x >> 3][x & 7] = (T)e_[x];  // rounded for the second product only, as above
+    };
 #pragma unroll
-    for (int u = 0; u < STEPS; ++u) {
-      if (u < 2 * DT) o[u % DT] = M::mma32(vb[v_at[2 * (1 - c) + u / DT] + (u % DT) * 32 * 8], pend[u / DT], o[u % DT]);
-      if (u < KS) behind = M::mma32(kb[k_at[u]], qf[u], behind);
+    for (int u = 0; u < AHEAD; ++u) read(u);
 #pragma unroll
-      for (int x = u * 16 / STEPS; x < (u + 1) * 16 / STEPS; ++x) {
-        const float e = exp2_fast(fmaf(sc[x], scale, sub));
-        if (x & 1) l1 += e; else l0 += e;
-        pf[x >> 3][x & 7] = (T)e;  // rounded for the second product only, as above
+    for (int u = 0; u < N; ++u) {
+      __builtin_amdgcn_sched_barrier(0);
+      const int i = u >> 1;
+      if (u & 1) behind = M::mma32(f_[u], qf[i], behind);
+      else o[i % DT] = M::mma32(f_[u], pend[i / DT], o[i % DT]);
+      if (u + AHEAD < N) read(u + AHEAD);
+#pragma unroll
+      for (int x = u * 16 / N; x < (u + 1) * 16 / N; ++x) {
+        e_[x] = exp2_fast(fmaf(sc[x], scale, sub));
+        if (x) rest(x - 1);  // the result of an exponential is not there at once
       }
     }
-    // Put the exponentials between the products (left alone, they sink behind the next branch): the
-    // operands' reads run ahead by four, then a product, a read and an element in turn.
+    rest(15);
     l0 += l1;
     asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l0));
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-    for (int u = 0; u < KS + 2 * DT; ++u) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
-    }
+    __builtin_amdgcn_sched_barrier(0);
     l += l0;
     if (moved)
 #pragma unroll
@@ -600,52 +682,54 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
   const std::integral_constant<int, 0> c0;
   const std::integral_constant<int, 1> c1;
 
-  Pages now = pages_of(0), next = pages_of(1), then = pages_of(2);
+  Pages now = uniform(ids_of(0)), next = uniform(ids_of(1)), then = ids_of(2);
   if (tiles) {
-    load_k(0, now, 0);
-    load_v(0, now, 0);
-    if (tiles > 1) load_k(1, next, 1);
-    // the first group has no group before: zeros times zero
-    for (uint32_t i = tid; i < D * 8u; i += kBlock) vt[1][i] = (v8)(T)0.0f;
+    load_k(0, now, kt0);
+    load_v(0, now, vt0);
+    if (tiles > 1) load_k(1, next, kt1);
+    // in the place of the values before the first tile's, which the first group takes: zeros times zero
+    for (uint32_t i = tid; i < VB / 16u; i += 64u * WAVES) ((v8*)vt1)[i] = (v8)(T)0.0f;
     landed();
 #pragma unroll
-    for (int k = 0; k < KS; ++k) sc = M::mma32(kt[0][k_at[k]], qf[k], sc);
+    for (int k = 0; k < KS; ++k) sc = M::mma32(k_piece(kt0, k, 0), qf[k], sc);
   }
   // Tile t: its first group while V of tile t - 1 and K of tile t are there; then everybody is done with
   // both, and V of tile t + 1 and K of tile t + 2 take their places.
-  const auto body = [&](auto buf_, int32_t t) __attribute__((always_inline)) {
-    constexpr uint32_t buf = decltype(buf_)::value;
-    if (t < wave_tiles) group(c0, t, now, vt[buf ^ 1u], kt[buf] + 32 * CH);
+  const auto body = [&](auto odd_, int32_t t) __attribute__((always_inline)) {
+    constexpr bool odd = decltype(odd_)::value;
+    char *const k_now = odd ? kt1 : kt0, *const k_next = odd ? kt0 : kt1;
+    char *const v_now = odd ? vt1 : vt0, *const v_before = odd ? vt0 : vt1;
+    if (t < wave_tiles) group(c0, t, now, v_before, k_now);
     landed();
-    if (t + 1 < tiles) load_v(t + 1, next, buf ^ 1u);
-    if (t + 2 < tiles) load_k(t + 2, then, buf);
+    if (t + 1 < tiles) load_v(t + 1, next, v_before);
+    const Pages behind = uniform(then);
+    if (t + 2 < tiles) load_k(t + 2, behind, k_now);
+    then = ids_of(t + 3);
     const int32_t base = start + 64 * t;
     if ((now.x[0] | now.x[1] | now.x[2] | now.x[3]) < 0 || base + 64 > q.len) {
-      for (uint32_t i = tid; i < D * 8u; i += kBlock) {  // what is not an entry may hold anything
-        const uint32_t part = (i & 7u) ^ spread<8>(i >> 3);
+      for (uint32_t i = tid; i < D * 8u; i += 64u * WAVES) {  // what is not an entry may hold anything
+        const uint32_t part = (i & 7u) ^ turn<8>(i >> 3);
         const int32_t run = part & 4u ? (part & 2u ? now.x[3] : now.x[2]) : (part & 2u ? now.x[1] : now.x[0]);
-        v8 x = vt[buf][i];
-#pragma unroll
+        v8 x = *(const v8*)(v_now + i / 64u * kRun + i % 64u * 16u);
         for (int y = 0; y < 8; ++y)
           if (run < 0 || base + (int32_t)(8 * part) + y >= q.len) x[y] = (T)0.0f;
-        vt[buf][i] = x;
+        *(v8*)(v_now + i / 64u * kRun + i % 64u * 16u) = x;
       }
       __syncthreads();
     }
     if (t < wave_tiles) {
-      group(c1, t, now, vt[buf], kt[buf ^ 1u]);
+      group(c1, t, now, v_now, k_next);
       if (t + 1 == wave_tiles)
 #pragma unroll
         for (int u = 0; u < 2 * DT; ++u)
-          o[u % DT] = M::mma32(vt[buf][v_at[2 + u / DT] + (u % DT) * 32 * 8], pend[u / DT], o[u % DT]);
+          o[u % DT] = M::mma32(v_piece(v_now, 2 + u / DT, u % DT), pend[u / DT], o[u % DT]);
     }
     now = next;
-    next = then;
-    then = pages_of(t + 3);
+    next = behind;
   };
   for (int32_t t = 0; t < tiles; t += 2) {
-    body(std::integral_constant<uint32_t, 0>{}, t);
-    if (t + 1 < tiles) body(std::integral_constant<uint32_t, 1>{}, t + 1);
+    body(std::false_type{}, t);
+    if (t + 1 < tiles) body(std::true_type{}, t + 1);
   }
   l += __shfl_xor(l, 32);
   if (!is) return;
@@ -674,17 +758,18 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_many_kernel(Attn 
 
 // weight = decay * weight + the sum of p over a sequence's rows, which another product of the keys with
 // the queries gives, the entries in the lanes now and the rows in their registers: 64 entries a wavefront
-// with their keys in registers, 64 rows at a time from double-buffered LDS.  Bound by the exponentials.
+// with their keys in registers, 64 rows at a time from double-buffered LDS.  As above, the exponentials of
+// 32 rows run beside the products of the next 32; the two take about the same time.
 constexpr uint32_t kWeightKeys = 256, kWeightRows = 64;
 
 template <typename M, int D>
 __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kernel(Attn p, float decay) {
   typedef typename M::t T;
   typedef typename M::v8 v8;
-  constexpr uint32_t CH = D / 8;
+  constexpr uint32_t CH = D / 8, QB = kWeightRows * D * 2 / 1024 * kRun;
   constexpr int KS = D / 16, NQ = CH / 4;
-  __shared__ v8 qt[2][kWeightRows * CH];
-  __shared__ f32x4 base[2][kWeightRows / 4];  // minus the rows' log sums, in powers of two
+  __shared__ alignas(16) char qt0[QB], qt1[QB];
+  __shared__ f32x4 base[4][kWeightRows / 4];  // minus the rows' log sums, in powers of two, of tile t in t % 4
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 63u, half = lane >> 5, c32 = lane & 31u;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
@@ -697,28 +782,34 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kerne
   const bool negate = p.scale2 < 0.0f;
   v8 kf[2][KS];
   int32_t page[2];
+#pragma unroll
   for (int y = 0; y < 2; ++y) {
     const int32_t e = mine + 32 * y + (int32_t)c32;
     page[y] = e < q.len ? kv_page(a, q, e >> a.page_bits) : -1;
     const T* key = (const T*)a.k + kv_base(a, page[y] < 0 ? 0 : page[y], h) + (size_t)((uint32_t)e & (a.page - 1u)) * D;
+#pragma unroll
     for (int k = 0; k < KS; ++k) kf[y][k] = signed_row(*(const v8*)(key + 16 * k + 8 * half), negate);
   }
   // rows of tokens before entry `first` see nothing here
   const uint32_t from = first > old ? ((uint32_t)(first - old) * a.group) & ~(kWeightRows - 1u) : 0u;
   const int32_t tiles = from < rows ? (int32_t)((rows - from + kWeightRows - 1u) / kWeightRows) : 0;
+  // the first tile with a row that sees an entry of the wavefront
+  const int32_t begin = mine > old ? (int32_t)(((uint32_t)(mine - old) * a.group - from) / kWeightRows) : 0;
   // token and head of the lane's rows of the next tile, moved on without dividing
   const uint32_t dj = kWeightRows / a.group, dg = kWeightRows % a.group;
-  uint32_t rj[NQ], rg[NQ], bj = 0, bg = 0;
+  uint32_t rj[NQ], rg[NQ], part[NQ], bj = 0, bg = 0;
+#pragma unroll
   for (int i = 0; i < NQ; ++i) {
-    const uint32_t r = from + ((wave * NQ + i) * 64u + lane) / CH;
-    rj[i] = r / a.group;
-    rg[i] = r % a.group;
+    const uint32_t c = (wave * NQ + i) * 64u + lane, row = c / CH;
+    rj[i] = (from + row) / a.group;
+    rg[i] = (from + row) % a.group;
+    part[i] = 8 * ((c % CH) ^ turn<CH>(row));
   }
   if (tid < kWeightRows) {
     bj = (from + tid) / a.group;
     bg = (from + tid) % a.group;
   }
-  const auto on = [&](uint32_t& j, uint32_t& g) {
+  const auto on = [&](uint32_t& j, uint32_t& g) __attribute__((always_inline)) {
     j += dj;
     g += dg;
     if (g >= a.group) {
@@ -726,71 +817,119 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kerne
       ++j;
     }
   };
-  const auto load = [&](uint32_t buf) {
+  const auto load = [&](char* qt) __attribute__((always_inline)) {
+#pragma unroll
     for (int i = 0; i < NQ; ++i) {
-      const uint32_t at = (wave * NQ + i) * 64u, c = at + lane, row = c / CH, part = (c % CH) ^ spread<CH>(row);
       const uint32_t j = rj[i] < (uint32_t)q.n ? rj[i] : (uint32_t)q.n - 1u;  // a row behind the last counts nothing
-      to_lds((const T*)p.q.p + (size_t)(q.t0 + (int32_t)j) * p.q.tok + (h * a.group + rg[i]) * p.q.head + 8 * part,
-             &qt[buf][at]);
+      to_lds((const T*)p.q.p + (size_t)(q.t0 + (int32_t)j) * p.q.tok + (h * a.group + rg[i]) * p.q.head + part[i],
+             qt + (wave * NQ + i) * kRun);
       on(rj[i], rg[i]);
     }
   };
   float b = 0.0f;
-  const auto load_base = [&] {
+  const auto load_base = [&]() __attribute__((always_inline)) {
     if (tid < kWeightRows) {
       b = bj < (uint32_t)q.n ? p.lse[(size_t)(q.t0 + (int32_t)bj) * a.n_q + h * a.group + bg] : kInf;
       on(bj, bg);
     }
   };
-  const auto put_base = [&](uint32_t buf) {  // a row that sees nothing has -inf
-    if (tid < kWeightRows) ((float*)base[buf])[tid] = b == -kInf ? -kInf : b * -kLog2e;
+  const auto put_base = [&](int32_t t) __attribute__((always_inline)) {  // a row that sees nothing has -inf
+    if (tid < kWeightRows) ((float*)base[t & 3])[tid] = b == -kInf ? -kInf : b * -kLog2e;
+  };
+  uint32_t q_at[2];
+  q_at[0] = piece_at<CH>(c32, half);
+  q_at[1] = piece_at<CH>(c32, 2 + half);
+  const auto piece = [&](const char* qt, int k, uint32_t x) __attribute__((always_inline)) {
+    return *(const v8*)(qt + q_at[k & 1] + (k >> 1) * 64 + x * (32 * CH / 64) * kRun);
   };
   float sum[2] = {0.0f, 0.0f};
+  f32x16 sc[2];
+  sc[0] = sc[1] = (f32x16)0.0f;
+  // Rows 32 x to 32 x + 31 of tile t, their scores in sc; the next rows' from `qt`, rows 32 (1 - x) on.
+  const auto rows32 = [&](auto x_, auto whole_, int32_t t, const char* qt) __attribute__((always_inline)) {
+    constexpr int x = decltype(x_)::value;
+    constexpr bool whole = decltype(whole_)::value;
+    constexpr int N = 2 * KS, AHEAD = 3, PER = 32 / N;
+    f32x4 n[4];  // register i is row 8 (i / 4) + 4 half + i % 4 of the 32
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) n[i] = base[t & 3][8 * x + 2 * i + half];
+    // entry e is seen from row (e - old) * group on
+    int32_t behind[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+      behind[y] = (int32_t)(from + (uint32_t)t * kWeightRows + 32u * x + 4u * half) -
+                  (mine + 32 * y + (int32_t)c32 > old ? (mine + 32 * y + (int32_t)c32 - old) * (int32_t)a.group : 0);
+    f32x16 nx[2];
+    nx[0] = nx[1] = (f32x16)0.0f;
+    v8 f_[KS];
+    float e_[32], part[2] = {0.0f, 0.0f};  // a tile's sums first: thousands of rows added one by one would lose bits
+    const auto add = [&](int z) __attribute__((always_inline)) {
+      const int y = z >> 4, i = z & 15;
+      part[y] += whole || behind[y] + 8 * (i >> 2) + (i & 3) >= 0 ? e_[z] : 0.0f;
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) f_[k] = piece(qt, k, 1 - x);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      __builtin_amdgcn_sched_barrier(0);
+      nx[u & 1] = M::mma32(f_[u >> 1], kf[u & 1][u >> 1], nx[u & 1]);
+      if (!(u & 1) && (u >> 1) + AHEAD < KS) f_[(u >> 1) + AHEAD] = piece(qt, (u >> 1) + AHEAD, 1 - x);
+#pragma unroll
+      for (int z = u * PER; z < (u + 1) * PER; ++z) {
+        e_[z] = exp2_fast(fmaf(sc[z >> 4][z & 15], scale, n[(z & 15) >> 2][z & 3]));
+        asm volatile("" : "+v"(e_[z]));  // here, not in pairs behind the products
+        if (z) add(z - 1);
+      }
+    }
+    add(31);
+    asm volatile("" : "+v"(part[0]), "+v"(part[1]));
+    __builtin_amdgcn_sched_barrier(0);
+    sum[0] += part[0];
+    sum[1] += part[1];
+    sc[0] = nx[0];
+    sc[1] = nx[1];
+  };
+  const auto step = [&](auto x_, int32_t t, const char* qt) __attribute__((always_inline)) {
+    const uint32_t r = from + (uint32_t)t * kWeightRows + 32u * decltype(x_)::value;
+    if (old + (int32_t)(r / a.group) + 1 >= mine + 64) rows32(x_, std::true_type{}, t, qt);
+    else rows32(x_, std::false_type{}, t, qt);
+  };
+  const std::integral_constant<int, 0> x0;
+  const std::integral_constant<int, 1> x1;
   if (tiles) {
-    load(0);
+    load(qt0);
     load_base();
-  }
-  for (int32_t t = 0; t < tiles; ++t) {
-    const uint32_t buf = (uint32_t)t & 1u, r0 = from + (uint32_t)t * kWeightRows;
-    put_base(buf);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    put_base(0);
+    if (tiles > 1) {
+      load(qt1);
+      load_base();
+      put_base(1);
+    }
+    wait_loads();
     __syncthreads();
-    if (t + 1 < tiles) {
-      load(buf ^ 1u);
+#pragma unroll
+    for (int u = 0; u < 2 * KS; ++u) sc[u & 1] = M::mma32(piece(qt0, u >> 1, 0), kf[u & 1][u >> 1], sc[u & 1]);
+  }
+  // Tile t: its first 32 rows while its second 32 are there; then everybody is done with its queries, and tile
+  // t + 2 takes their place.  Scores are made one step ahead, so a wavefront begins a tile early.
+  const auto body = [&](auto odd_, int32_t t) __attribute__((always_inline)) {
+    constexpr bool odd = decltype(odd_)::value;
+    char *const qt = odd ? qt1 : qt0, *const qt_next = odd ? qt0 : qt1;
+    if (t + 1 >= begin) step(x0, t, qt);
+    wait_loads();
+    __syncthreads();
+    if (t + 2 < tiles) {
+      load(qt);
       load_base();
     }
-    const uint32_t last = r0 + kWeightRows - 1u < rows ? r0 + kWeightRows - 1u : rows - 1u;
-    if (old + (int32_t)(last / a.group) + 1 <= mine) continue;  // its rows see none of the wavefront's entries
-    const bool whole = old + (int32_t)(r0 / a.group) + 1 >= mine + 64;
-    for (uint32_t x = 0; x < 2; ++x) {
-      f32x16 sc[2];
-      sc[0] = sc[1] = (f32x16)0.0f;
-      for (int k = 0; k < KS; ++k) {
-        const uint32_t row = 32u * x + c32;
-        const v8 f = qt[buf][row * CH + ((2 * k + half) ^ spread<CH>(row))];
-        sc[0] = M::mma32(f, kf[0][k], sc[0]);
-        sc[1] = M::mma32(f, kf[1][k], sc[1]);
-      }
-      f32x4 n[4];  // register i is row 8 (i / 4) + 4 half + i % 4 of the 32
-      for (uint32_t i = 0; i < 4; ++i) n[i] = base[buf][8 * x + 2 * i + half];
-      for (int y = 0; y < 2; ++y) {
-        float part = 0.0f;  // a tile's sum first: thousands of rows added one by one would lose bits
-        if (whole) {
-          for (int i = 0; i < 16; ++i) part += exp2_fast(fmaf(sc[y][i], scale, n[i >> 2][i & 3]));
-        } else {
-          const int32_t e = mine + 32 * y + (int32_t)c32;
-          for (int i = 0; i < 16; ++i) {
-            const uint32_t r = r0 + 32u * x + 8u * (i >> 2) + 4u * half + (i & 3);
-            // entry e is seen from row (e - old) * group on
-            const bool sees = (int64_t)r >= (int64_t)(e - old) * (int64_t)a.group;
-            const float v = exp2_fast(fmaf(sc[y][i], scale, n[i >> 2][i & 3]));
-            part += sees ? v : 0.0f;
-          }
-        }
-        sum[y] += part;
-      }
-    }
+    if (t + 1 >= begin) step(x1, t, qt_next);
+    if (t + 2 < tiles) put_base(t + 2);
+  };
+  for (int32_t t = 0; t < tiles; t += 2) {
+    body(std::false_type{}, t);
+    if (t + 1 < tiles) body(std::true_type{}, t + 1);
   }
+#pragma unroll
   for (int y = 0; y < 2; ++y) {
     sum[y] += __shfl_xor(sum[y], 32);
     if (page[y] < 0 || half) continue;
@@ -852,7 +991,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.few_split = (a.max_len + p.few_chunk - 1) / p.few_chunk;
     p.few_cap = (uint32_t)(row_most < kRowsFew ? row_most : kRowsFew);
     if (p.many) {
-      const uint64_t row_tiles = (row_most + kManyRows - 1) / kManyRows;
+      const uint64_t row_tiles = (row_most + many_rows(a.dim) - 1) / many_rows(a.dim);
       p.many_chunk = chunk_of(a, a.max_len, pairs * row_tiles, 512, 512);
       p.many_split = (a.max_len + p.many_chunk - 1) / p.many_chunk;
     }
@@ -926,7 +1065,9 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.row_cap = row_most;
     p.rows_from = kRowsFew;
     p.rows_to = row_most;
-    launch(kv_many_kernel<M, D>, dim3(a.n_kv * plan.many_split, (row_most + kManyRows - 1) / kManyRows, a.n_seq));
+    hipLaunchKernelGGL((kv_many_kernel<M, D>),
+                       dim3(a.n_kv * plan.many_split, (row_most + many_rows(D) - 1) / many_rows(D), a.n_seq),
+                       dim3(64 * many_waves(D)), 0, st, p);
     if (plan.many_split > 1) join(row_most);
     if (weights) launch(kv_weight_many_kernel<M, D>, dim3((a.max_len + kWeightKeys - 1) / kWeightKeys, a.n_kv, a.n_seq),
                         decay);
@@ -947,7 +1088,7 @@ bool kv_attend_fits(const KvArgs& a, uint32_t n_sel) {
     const uint64_t tiles = (a.group + p.few_rows - 1) / p.few_rows, scored = (a.max_len >> a.page_bits) / 64 + 1;
     return p.few_split * tiles * a.max_new <= most && scored * a.max_new <= most;
   }
-  return (uint64_t)a.n_kv * p.many_split <= most && (rows + kManyRows - 1) / kManyRows <= 65535;
+  return (uint64_t)a.n_kv * p.many_split <= most && rows / many_rows(a.dim) < 65535;
 }
 
 hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, uint32_t n_sel, uint32_t first, uint32_t last,
