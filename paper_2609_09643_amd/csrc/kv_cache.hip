@@ -176,6 +176,7 @@ struct Pick {
   uint32_t hist[2048];
   uint32_t sums[2][BLOCK / 64];
   uint32_t found[3];
+  unsigned long long best;
 };
 
 template <int BLOCK, int PER>
@@ -302,9 +303,11 @@ __device__ void pick_chosen(const uint32_t (&key)[PER], uint32_t count, Cut cut,
 
 // ------------------------------------------------------------------ victims
 
+constexpr uint32_t kFewVictims = 4;  // up to which rounds of a minimum beat the digits' histograms
+
 // One block per (kv head, sequence) of up to BLOCK * PER entries: weights and positions are read once.
 template <int BLOCK, int PER>
-__global__ __launch_bounds__(BLOCK) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
+__global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
                                                            uint32_t recent, uint32_t max_evict,
                                                            int32_t* victims, int32_t* src, int32_t* new_len) {
   __shared__ Pick<BLOCK, PER> s;
@@ -349,6 +352,51 @@ __global__ __launch_bounds__(BLOCK) void kv_victims_kernel(KvArgs a, uint32_t bu
     const int64_t newest = (int64_t)top - (int64_t)recent;
     for (int i = 0; i < PER; ++i)
       if (pos[i] < (int64_t)first || pos[i] > newest) key[i] = 0xFFFFFFFFu;
+    if (PER < 32 && n <= kFewVictims) {  // a step's victim or two: the smallest of key and slot, one after the other
+      int32_t gone[kFewVictims];
+      uint64_t last = 0;
+      for (uint32_t v = 0; v < kFewVictims; ++v) gone[v] = INT32_MAX;
+      for (uint32_t v = 0; v < n; ++v) {
+        uint64_t best = ~0ull;
+        for (int i = 0; i < PER; ++i) {
+          const uint32_t e = pick_number<BLOCK, PER>(i);
+          const uint64_t x = ((uint64_t)key[i] << 32) | e;
+          if (e < len && (v == 0 || x > last) && x < best) best = x;
+        }
+        if (tid == 0) s.best = ~0ull;
+        __syncthreads();
+        atomicMin(&s.best, (unsigned long long)best);
+        __syncthreads();
+        last = s.best;
+        __syncthreads();
+        // in the order of slots
+        int32_t e = (int32_t)(uint32_t)last;
+        for (uint32_t w = 0; w < kFewVictims; ++w) {
+          const int32_t x = gone[w];
+          gone[w] = e < x ? e : x;
+          e = e < x ? x : e;
+        }
+      }
+      if (tid < max_evict) {
+        int32_t mine = -1, from = -1;
+        if (tid < n) {
+          uint32_t filled = 0;
+          for (uint32_t e = stay; e < len; ++e) {
+            bool is = false;
+            for (uint32_t w = 0; w < kFewVictims; ++w) is = is || gone[w] == (int32_t)e;
+            if (!is) {
+              if (filled == tid) from = (int32_t)e;
+              ++filled;
+            }
+          }
+          for (uint32_t w = 0; w < kFewVictims; ++w) mine = w == tid ? gone[w] : mine;
+        }
+        victims[row + tid] = mine;
+        src[row + tid] = from;
+      }
+      for (uint32_t i = BLOCK + tid; i < max_evict; i += BLOCK) victims[row + i] = src[row + i] = -1;
+      return;
+    }
     const Cut cut = pick_cut<BLOCK, PER>(key, n, s);
     bool out[PER], fill[PER];
     uint32_t at[PER];
@@ -702,7 +750,7 @@ __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, u
 }
 
 template <int BLOCK, int PER>
-__global__ __launch_bounds__(BLOCK) void kv_choose_kernel(KvArgs a, uint32_t n_sel, const uint32_t* keys,
+__global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_choose_kernel(KvArgs a, uint32_t n_sel, const uint32_t* keys,
                                                           int32_t* sel) {
   __shared__ Pick<BLOCK, PER> s;
   const uint32_t h = blockIdx.y, j = blockIdx.x, tid = threadIdx.x;
@@ -759,8 +807,8 @@ hipError_t with_type(const KvArgs& a, F f) {
 template <typename F>
 bool with_pick(uint32_t n, F f) {
   if (n <= 1024) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
-  else if (n <= 4096) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
-  else if (n <= 8192) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 16>{});
+  else if (n <= 4096) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+  else if (n <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 8>{});
   else if (n <= 16384) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 16>{});
   else if (n <= 32768) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 32>{});
   else return false;
