@@ -179,10 +179,17 @@ struct Pick {
   unsigned long long best;
 };
 
-template <int BLOCK, int PER>
-__device__ __forceinline__ uint32_t pick_number(int i) {
-  return (threadIdx.x >> 6) * 64u * PER + (uint32_t)(i / 4) * 256u + 4u * (threadIdx.x & 63u) + (uint32_t)(i % 4);
-}
+struct Numbers {
+  uint32_t base;
+  template <int PER>
+  static __device__ __forceinline__ Numbers of() {
+    return Numbers{(threadIdx.x >> 6) * 64u * PER + 4u * (threadIdx.x & 63u)};
+  }
+  __device__ __forceinline__ uint32_t operator()(int i) const { return base + (uint32_t)(i / 4) * 256u + (uint32_t)(i % 4); }
+  // Made anew where a new pass begins: kept from the first one, the numbers and what was compared with them
+  // take more registers than the keys.
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(base)); }
+};
 
 struct Cut {
   uint32_t key;   // the largest chosen key
@@ -190,18 +197,20 @@ struct Cut {
 };
 
 // The cut of the `need` smallest keys, 1 <= need <= the keys' count; a key of 0xFFFFFFFF is chosen only when
-// the others do not suffice, and elements at and past `count` hold it.  Digits of 11, 11 and 10 bits from
+// the others do not suffice, and elements at and past the keys' count hold it.  Digits of 11, 11 and 10 bits from
 // the top: a histogram (whole numbers: any order of additions gives the same), its prefix, and the
 // digit the cut is in.  It ends early once a digit is taken whole.
 template <int BLOCK, int PER>
-__device__ Cut pick_cut(const uint32_t (&key)[PER], uint32_t need, Pick<BLOCK, PER>& s) {
+__device__ __forceinline__ Cut pick_cut(const uint32_t (&key)[PER], uint32_t need, Pick<BLOCK, PER>& s) {
   constexpr uint32_t BINS = 2048 / BLOCK;
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
   for (uint32_t i = 0; i < BINS; ++i) s.hist[tid * BINS + i] = 0;
   uint32_t prefix = 0, left = need, top = 0;  // bits of the key at and above `top` are known
+#pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const uint32_t shift = pass == 0 ? 21u : pass == 1 ? 10u : 0u, mask = pass == 2 ? 1023u : 2047u;
     __syncthreads();
+#pragma unroll
     for (int i = 0; i < PER; ++i) {
       const bool in = key[i] != 0xFFFFFFFFu && (pass == 0 || (key[i] >> top) == (prefix >> top));
       const uint32_t bin = (key[i] >> shift) & mask;
@@ -256,49 +265,68 @@ __device__ Cut pick_cut(const uint32_t (&key)[PER], uint32_t need, Pick<BLOCK, P
   return Cut{prefix, left};
 }
 
-// Places of flagged elements in the order of their numbers: at[i] for element i, and the block's total.
-template <int BLOCK, int PER>
-__device__ uint32_t pick_places(const bool (&flag)[PER], uint32_t (&at)[PER], uint32_t* sums) {
+// Calls emit(i, place) for the flagged elements, their places in the order of their numbers; the block's
+// total.  Of up to 32 elements the wavefront's flags stay in scalar registers; more are taken twice.
+template <int BLOCK, int PER, typename Flag, typename Emit>
+__device__ __forceinline__ uint32_t pick_places(Flag flag, Emit emit, uint32_t* sums) {
+  constexpr bool KEEP = PER <= 32;
   const uint32_t wave = threadIdx.x >> 6;
+  uint64_t kept[KEEP ? PER : 1];
   uint32_t n = 0;
-  for (int c = 0; c < PER / 4; ++c) {
-    uint32_t below = 0, total = 0;
-    for (int i = 0; i < 4; ++i) {
-      const uint64_t w = __builtin_amdgcn_ballot_w64(flag[4 * c + i]);
-      below += __builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0u));
-      total += (uint32_t)__builtin_popcountll(w);
-    }
-    uint32_t x = n + below;
-    for (int i = 0; i < 4; ++i) {
-      at[4 * c + i] = x;
-      x += flag[4 * c + i] ? 1u : 0u;
-    }
-    n += total;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint64_t w = __builtin_amdgcn_ballot_w64(flag(i));
+    if (KEEP) kept[KEEP ? i : 0] = w;
+    n += (uint32_t)__builtin_popcountll(w);
   }
   if ((threadIdx.x & 63u) == 0u) sums[wave] = n;
   __syncthreads();
-  uint32_t before = 0, all = 0;
+  uint32_t at = 0, all = 0;
   for (uint32_t w = 0; w < BLOCK / 64; ++w) {
-    before += w < wave ? sums[w] : 0u;
+    at += w < wave ? sums[w] : 0u;
     all += sums[w];
   }
-  for (int i = 0; i < PER; ++i) at[i] += before;
+  const uint64_t below = (1ull << (threadIdx.x & 63u));
+#pragma unroll
+  for (int c = 0; c < PER / 4; ++c) {
+    uint32_t x = at;
+    bool is[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t w = KEEP ? kept[KEEP ? 4 * c + i : 0] : __builtin_amdgcn_ballot_w64(flag(4 * c + i));
+      x += __builtin_amdgcn_mbcnt_hi((uint32_t)(w >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)w, 0u));
+      at += (uint32_t)__builtin_popcountll(w);
+      is[i] = (w & below) != 0ull;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (is[i]) emit(4 * c + i, x++);
+  }
   __syncthreads();
   return all;
 }
 
-// Which elements the cut chooses.
+// A bit for each of a thread's elements.
+template <int PER>
+struct Bits {
+  uint32_t w[(PER + 31) / 32];
+  __device__ __forceinline__ bool operator()(int i) const { return (w[i / 32] >> (i % 32)) & 1u; }
+  __device__ __forceinline__ void set(int i, bool x) { w[i / 32] |= (x ? 1u : 0u) << (i % 32); }
+  __device__ __forceinline__ void drop(int i) { w[i / 32] &= ~(1u << (i % 32)); }
+};
+
+// Which elements the cut chooses: at least as many keys as it takes, so never an element past the last key.
 template <int BLOCK, int PER>
-__device__ void pick_chosen(const uint32_t (&key)[PER], uint32_t count, Cut cut, bool (&out)[PER],
-                            Pick<BLOCK, PER>& s) {
-  for (int i = 0; i < PER; ++i) out[i] = pick_number<BLOCK, PER>(i) < count && key[i] <= cut.key;
-  if (cut.ties == 0xFFFFFFFFu) return;
-  bool tie[PER];
-  uint32_t at[PER];
-  for (int i = 0; i < PER; ++i) tie[i] = out[i] && key[i] == cut.key;
-  const uint32_t ties = pick_places<BLOCK, PER>(tie, at, s.sums[0]);
-  if (ties == cut.ties) return;
-  for (int i = 0; i < PER; ++i) out[i] = out[i] && (!tie[i] || at[i] < cut.ties);
+__device__ __forceinline__ Bits<PER> pick_chosen(const uint32_t (&key)[PER], Cut cut, Pick<BLOCK, PER>& s) {
+  Bits<PER> out = {};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) out.set(i, key[i] <= cut.key);
+  if (cut.ties != 0xFFFFFFFFu) {
+    const Bits<PER> before = out;
+    pick_places<BLOCK, PER>([&](int i) { return before(i) && key[i] == cut.key; },
+                            [&](int i, uint32_t at) { if (at >= cut.ties) out.drop(i); }, s.sums[0]);
+  }
+  return out;
 }
 
 // ------------------------------------------------------------------ victims
@@ -322,25 +350,37 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvA
   const size_t row = ((size_t)seq * a.n_kv + h) * max_evict;
   uint32_t got = 0, moved = 0;
   if (n) {
+    // the highest position first; more than 32 a thread are read again rather than kept
+    constexpr bool KEEP = PER <= 32;
     uint32_t key[PER];
-    int32_t pos[PER];
+    i32x4 pos[KEEP ? PER / 4 : 1];
     int32_t top = INT32_MIN;
+    Numbers num = Numbers::of<PER>();
+    // the word of entry e, any word for one that is not there
+    const auto word = [&](uint32_t e, bool& in) __attribute__((always_inline)) {
+      const int32_t p = kv_page(a, q, (int32_t)((e < len ? e : len - 1u) >> a.page_bits));
+      in = e < len && p >= 0;
+      return kv_word(a, p < 0 ? 0 : p, h) + (e & (a.page - 1u));
+    };
+#pragma unroll
     for (int c = 0; c < PER / 4; ++c) {
-      const uint32_t e = pick_number<BLOCK, PER>(4 * c);
-      const int32_t p = e < len ? kv_page(a, q, (int32_t)(e >> a.page_bits)) : -1;
-      f32x4 w = (f32x4)0.0f;
+      const uint32_t e = num(4 * c);
+      bool in = false;
       i32x4 x = (i32x4)0;
-      if (p >= 0) {
-        const size_t at = kv_word(a, p, h) + (e & (a.page - 1u));
-        w = *(const f32x4*)(a.weight + at);
+      f32x4 w = (f32x4)0.0f;
+      if (__builtin_amdgcn_ballot_w64(e < len)) {  // a wavefront behind the end reads nothing
+        const size_t at = word(e, in);
         x = *(const i32x4*)(a.pos + at);
+        w = *(const f32x4*)(a.weight + at);
       }
+      if (KEEP) pos[KEEP ? c : 0] = x;
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool in = p >= 0 && e + i < len;
-        key[4 * c + i] = in ? kv_order(w[i]) : 0xFFFFFFFFu;
-        pos[4 * c + i] = x[i];
-        if (in) top = x[i] > top ? x[i] : top;
+        const bool is = in && e + i < len;
+        key[4 * c + i] = is ? kv_order(w[i]) : 0xFFFFFFFFu;
+        top = is && x[i] > top ? x[i] : top;
       }
+      if (!KEEP && c % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // no more loads under way than registers
     }
     for (int o = 32; o; o >>= 1) {
       const int32_t y = __shfl_xor(top, o);
@@ -350,18 +390,27 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvA
     __syncthreads();
     for (uint32_t w = 0; w < BLOCK / 64; ++w) top = (int32_t)s.sums[1][w] > top ? (int32_t)s.sums[1][w] : top;
     const int64_t newest = (int64_t)top - (int64_t)recent;
-    for (int i = 0; i < PER; ++i)
-      if (pos[i] < (int64_t)first || pos[i] > newest) key[i] = 0xFFFFFFFFu;
-    if (PER < 32 && n <= kFewVictims) {  // a step's victim or two: the smallest of key and slot, one after the other
+    num.renew();
+#pragma unroll
+    for (int c = 0; c < PER / 4; ++c) {
+      bool in;
+      const i32x4 x = KEEP ? pos[KEEP ? c : 0] : *(const i32x4*)(a.pos + word(num(4 * c), in));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (x[i] < (int64_t)first || x[i] > newest) key[4 * c + i] = 0xFFFFFFFFu;
+      if (!KEEP && c % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    if (KEEP && n <= kFewVictims) {  // a step's victim or two: the smallest of key and slot, one after the other
       int32_t gone[kFewVictims];
       uint64_t last = 0;
       for (uint32_t v = 0; v < kFewVictims; ++v) gone[v] = INT32_MAX;
       for (uint32_t v = 0; v < n; ++v) {
         uint64_t best = ~0ull;
-        for (int i = 0; i < PER; ++i) {
-          const uint32_t e = pick_number<BLOCK, PER>(i);
-          const uint64_t x = ((uint64_t)key[i] << 32) | e;
-          if (e < len && (v == 0 || x > last) && x < best) best = x;
+        num.renew();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {  // what is no entry has the largest key and a larger number than any entry
+          const uint64_t x = ((uint64_t)key[i] << 32) | num(i);
+          if ((v == 0 || x > last) && x < best) best = x;
         }
         if (tid == 0) s.best = ~0ull;
         __syncthreads();
@@ -398,19 +447,12 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvA
       return;
     }
     const Cut cut = pick_cut<BLOCK, PER>(key, n, s);
-    bool out[PER], fill[PER];
-    uint32_t at[PER];
-    pick_chosen<BLOCK, PER>(key, len, cut, out, s);
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t e = pick_number<BLOCK, PER>(i);
-      fill[i] = e >= stay && e < len && !out[i];
-    }
-    got = pick_places<BLOCK, PER>(out, at, s.sums[0]);
-    for (int i = 0; i < PER; ++i)
-      if (out[i]) victims[row + at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
-    moved = pick_places<BLOCK, PER>(fill, at, s.sums[0]);
-    for (int i = 0; i < PER; ++i)
-      if (fill[i]) src[row + at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
+    const Bits<PER> out = pick_chosen<BLOCK, PER>(key, cut, s);
+    num.renew();
+    got = pick_places<BLOCK, PER>(out, [&](int i, uint32_t at) { victims[row + at] = (int32_t)num(i); }, s.sums[0]);
+    num.renew();
+    moved = pick_places<BLOCK, PER>([&](int i) { return num(i) >= stay && num(i) < len && !out(i); },
+                                    [&](int i, uint32_t at) { src[row + at] = (int32_t)num(i); }, s.sums[0]);
   }
   for (uint32_t i = got + tid; i < max_evict; i += BLOCK) victims[row + i] = -1;
   for (uint32_t i = moved + tid; i < max_evict; i += BLOCK) src[row + i] = -1;
@@ -764,20 +806,18 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_choose_kernel(KvAr
   uint32_t got = 0;
   if (count) {
     uint32_t key[PER];
-    bool take[PER];
+    Numbers num = Numbers::of<PER>();
+#pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint32_t o = pick_number<BLOCK, PER>(i);
-      key[i] = o < count ? in[o] : 0xFFFFFFFFu;
+      key[i] = in[num(i) < count ? num(i) : count - 1u];
+      key[i] = num(i) < count ? key[i] : 0xFFFFFFFFu;
     }
-    if (count > n_sel) {
-      const Cut cut = pick_cut<BLOCK, PER>(key, n_sel, s);
-      pick_chosen<BLOCK, PER>(key, count, cut, take, s);
-    }
-    for (int i = 0; i < PER; ++i) take[i] = (count <= n_sel || take[i]) && key[i] != 0xFFFFFFFFu;
-    uint32_t at[PER];
-    got = pick_places<BLOCK, PER>(take, at, s.sums[0]);
-    for (int i = 0; i < PER; ++i)
-      if (take[i]) out[at[i]] = (int32_t)pick_number<BLOCK, PER>(i);
+    Cut cut = {0xFFFFFFFEu, 0xFFFFFFFFu};  // every page that is there
+    if (count > n_sel) cut = pick_cut<BLOCK, PER>(key, n_sel, s);
+    const Bits<PER> take = pick_chosen<BLOCK, PER>(key, cut, s);
+    num.renew();
+    got = pick_places<BLOCK, PER>([&](int i) { return take(i) && key[i] != 0xFFFFFFFFu; },
+                                  [&](int i, uint32_t at) { out[at] = (int32_t)num(i); }, s.sums[0]);
   }
   for (uint32_t i = got + tid; i < n_sel; i += BLOCK) out[i] = -1;
 }
@@ -830,11 +870,14 @@ hipError_t launch_kv_victims(const KvArgs& a, uint32_t budget, uint32_t first, u
                              uint32_t max_evict, int32_t* victims, int32_t* src, int32_t* new_len,
                              hipStream_t st) {
   const dim3 grid(a.n_kv, a.n_seq);
-  if (!with_pick(a.max_len, [&](auto block, auto per) {
-        hipLaunchKernelGGL((kv_victims_kernel<decltype(block)::value, decltype(per)::value>), grid,
-                           dim3(decltype(block)::value), 0, st, a, budget, first, recent, max_evict, victims, src,
-                           new_len);
-      }))
+  const auto picked = [&](auto block, auto per) {
+    hipLaunchKernelGGL((kv_victims_kernel<decltype(block)::value, decltype(per)::value>), grid,
+                       dim3(decltype(block)::value), 0, st, a, budget, first, recent, max_evict, victims, src, new_len);
+  };
+  if (with_pick(a.max_len, picked)) return hipGetLastError();
+  if (a.max_len <= 65536)
+    picked(std::integral_constant<int, 1024>{}, std::integral_constant<int, 64>{});
+  else
     hipLaunchKernelGGL(kv_victims_long_kernel, grid, dim3(kSelBlock), 0, st, a, budget, first, recent, max_evict,
                        victims, src, new_len);
   return hipGetLastError();

@@ -63,6 +63,19 @@ def _torch():
     return torch
 
 
+_raw = None
+
+
+def _raw_stream(index):
+    """The current stream's handle; the Stream object around it takes as long to make as a launch."""
+    global _raw
+    if _raw is None:
+        torch = _torch()
+        _raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw(index)
+
+
 def _refuse(why):
     raise UnisonError(E_INVALID, why)
 
@@ -156,10 +169,11 @@ class _On:
         torch = _torch()
         if self.device.type != "cuda":
             _refuse("the operators run on the GPU, the pool is on %s" % self.device)
+        index = self.device.index
         self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
-            torch.cuda.set_device(self.device)
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        if self.before != index:
+            torch.cuda.set_device(index)
+        return _raw_stream(index)
 
     def __exit__(self, *exc):
         if self.before != self.device.index:
