@@ -84,8 +84,8 @@ int heads(KvArgs& a, uint32_t n_q) {
   if (n_q < 1 || n_q % a.n_kv || n_q / a.n_kv > kMaxGroup) return UNISON_E_INVALID;
   a.n_q = n_q;
   a.group = n_q / a.n_kv;
-  // rows of the token arrays are counted in 31 bits
-  return (uint64_t)a.n_tok * n_q > 0x7FFFFFFFull ? UNISON_E_CAPACITY : UNISON_OK;
+  // rows of a sequence, and a tile's behind them, are counted in 31 bits
+  return (uint64_t)a.n_tok * n_q > 1ull << 30 ? UNISON_E_CAPACITY : UNISON_OK;
 }
 
 int done(hipError_t rc) { return rc == hipSuccess ? UNISON_OK : UNISON_E_HIP; }

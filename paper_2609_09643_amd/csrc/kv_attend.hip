@@ -51,7 +51,6 @@ constexpr uint32_t kBlock = 256;
 constexpr uint32_t kWaves = kBlock / 64;
 constexpr uint32_t kRowsFew = 32;         // rows of a (sequence, kv head) up to which the few-rows kernel serves it
 constexpr uint32_t kPagesLds = 1024;      // page ids of one block's entries
-constexpr uint32_t kPagesPast = 64;       // and, of no pages, those of tiles read ahead
 constexpr uint32_t kManyKeys = 64;
 // The many-rows kernel: wavefronts of a block, 32 rows each, and tiles of 64 entries in LDS.
 constexpr uint32_t many_waves(uint32_t dim) { return dim <= 128 ? 8 : 4; }
@@ -70,8 +69,7 @@ struct Attn {
   float* lse;
   const int32_t* sel;   // [n_tok][n_kv][n_sel], or null: every page
   uint32_t n_sel;
-  // Partial results of a split of the entries, for row r of (sequence s, kv head h):
-  // index ((split * n_seq + s) * n_kv + h) * row_cap + r
+  // Partial results of a split of the entries (part_row)
   float* part_o;        // [..][dim], times the exponential of the maximum
   float2* part_ml;      // maximum (power of two) and sum
   float* scores;        // of the dense few-rows kernel (score_at), or null
@@ -82,8 +80,11 @@ struct Attn {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float or_zero(float m) { return m == -kInf ? 0.0f : m; }
 
-__device__ __forceinline__ size_t part_row(const Attn& p, uint32_t split, uint32_t s, uint32_t h) {
-  return (((size_t)split * p.a.n_seq + s) * p.a.n_kv + h) * p.row_cap;
+// Where the partial results of row r of (sequence, kv head) lie: few rows of every pair (row_cap of
+// them), or, where sequences may have many, the tokens' own rows (row_cap 0).
+__device__ __forceinline__ size_t part_row(const Attn& p, uint32_t split, uint32_t s, uint32_t h, int32_t t0, uint32_t r) {
+  if (p.row_cap) return (((size_t)split * p.a.n_seq + s) * p.a.n_kv + h) * p.row_cap + r;
+  return ((size_t)split * p.a.n_tok + (uint32_t)t0 + r / p.a.group) * p.a.n_q + h * p.a.group + r % p.a.group;
 }
 
 // Scores of row r and 32 entries, those 8 g + 4 x to + 3 of them in word g: rows side by side, so that the
@@ -301,7 +302,7 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
   for (int n = 0; n < NT; ++n) {
     const uint32_t r = r16 + 16u * n;
     if (r >= rows) continue;
-    const size_t part = part_row(p, split, s, h) + r0 + r;
+    const size_t part = part_row(p, split, s, h, q.t0, r0 + r);
     if (g4 == 0 && (p.n_split > 1 || SCORES)) p.part_ml[part] = make_float2(m[n], l[n]);
     if (p.n_split > 1) {
       for (int t = 0; t < DT; ++t) *(f32x4*)(p.part_o + part * D + 16 * t + 4 * g4) = o[n][t];
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
     f32x4 x[B];
     for (uint32_t i = 0; i < B; ++i) {
       const bool is = i0 + i < used;
-      const size_t part = part_row(p, is ? i0 + i : i0, s, h) + r;
+      const size_t part = part_row(p, is ? i0 + i : i0, s, h, q.t0, r);
       y[i] = p.part_ml[part];
       x[i] = *(const f32x4*)(p.part_o + part * D + d);
       if (!is) y[i] = make_float2(-kInf, 0.0f);
@@ -377,7 +378,7 @@ __global__ __launch_bounds__(kBlock) void kv_weight_few_kernel(Attn p, float dec
       float2 y[8];
       float next = m;
       for (uint32_t i = 0; i < 8; ++i) {
-        y[i] = p.part_ml[part_row(p, i0 + i < used ? i0 + i : i0, s, h) + tid];
+        y[i] = p.part_ml[part_row(p, i0 + i < used ? i0 + i : i0, s, h, q.t0, tid)];
         if (i0 + i >= used) y[i] = make_float2(-kInf, 0.0f);
         next = fmaxf(next, y[i].x);
       }
@@ -467,7 +468,7 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
   // an array for each buffer: the compiler waits for every load into an array before it reads the array
   constexpr uint32_t KB = kManyKeys * D * 2 / 1024 * kRun, VB = D * 128 / 1024 * kRun;
   __shared__ alignas(16) char kt0[KB], kt1[KB], vt0[VB], vt1[VB];
-  __shared__ int32_t pg[kPagesLds + kPagesPast];
+  __shared__ int32_t pg[kPagesLds];
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.x % a.n_kv, split = blockIdx.x / a.n_kv, s = blockIdx.z, tid = threadIdx.x;
   const uint32_t lane = tid & 63u, half = lane >> 5, r32 = lane & 31u;
@@ -514,21 +515,31 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
   const size_t head = (size_t)h * a.page * D, per_page = (size_t)a.n_kv * a.page * D;
   const uint32_t in_page = a.page - 1u;
   const bool wide = a.page >= kManyKeys;
-  // The page ids of the block's entries; a tile's are read a tile ahead of their use.
+  // The page ids of the next kPagesLds pages, from tile `ids_from` on (whole pages); a tile's are read a
+  // tile ahead of their use.
   const uint32_t n_ids = end > start ? (uint32_t)(end - start + (int32_t)in_page) >> a.page_bits : 0u;
-  for (uint32_t i = tid; i < n_ids + kPagesPast; i += 64u * WAVES)
-    pg[i] = i < n_ids ? kv_page(a, q, (int32_t)(((uint32_t)start >> a.page_bits) + i)) : -1;
-  __syncthreads();
+  const int32_t window = (int32_t)((kPagesLds << a.page_bits) / kManyKeys);
+  int32_t ids_from = 0;
+  const auto fill_ids = [&] {
+    const uint32_t first_id = (uint32_t)ids_from * kManyKeys >> a.page_bits;
+    for (uint32_t i = tid; i < kPagesLds; i += 64u * WAVES) {
+      const uint32_t id = first_id + i;
+      pg[i] = id < n_ids ? kv_page(a, q, (int32_t)(((uint32_t)start >> a.page_bits) + id)) : -1;
+    }
+    __syncthreads();
+  };
+  fill_ids();
   struct Pages {  // of a tile's four runs of 16 entries, x[0] of all where a page holds the tile
     int32_t x[4];
   };
   const auto ids_of = [&](int32_t t) __attribute__((always_inline)) {
     Pages to;
-    to.x[0] = pg[(uint32_t)(64 * t) >> a.page_bits];
+    const uint32_t e = (uint32_t)(t - ids_from) * kManyKeys;
+    to.x[0] = pg[e >> a.page_bits];
     to.x[1] = to.x[2] = to.x[3] = to.x[0];
     if (!wide)
 #pragma unroll
-      for (int i = 1; i < 4; ++i) to.x[i] = pg[(uint32_t)(64 * t + 16 * i) >> a.page_bits];
+      for (int i = 1; i < 4; ++i) to.x[i] = pg[(e + 16u * i) >> a.page_bits];
     return to;
   };
   const auto uniform = [&](const Pages& from) __attribute__((always_inline)) {
@@ -705,6 +716,10 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
     if (t + 1 < tiles) load_v(t + 1, next, v_before);
     const Pages behind = uniform(then);
     if (t + 2 < tiles) load_k(t + 2, behind, k_now);
+    if (t + 3 - ids_from >= window) {  // nobody reads the old ids any more: the last are in registers
+      ids_from = (t + 3) & ~3;         // pages of 256 hold four tiles
+      fill_ids();
+    }
     then = ids_of(t + 3);
     const int32_t base = start + 64 * t;
     if ((now.x[0] | now.x[1] | now.x[2] | now.x[3]) < 0 || base + 64 > q.len) {
@@ -734,7 +749,7 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
   }
   l += __shfl_xor(l, 32);
   if (!is) return;
-  const size_t part = part_row(p, split, s, h) + r;
+  const size_t part = part_row(p, split, s, h, q.t0, r);
   if (p.n_split > 1) {
     if (half == 0) p.part_ml[part] = make_float2(m, l);
 #pragma unroll
@@ -954,12 +969,11 @@ struct Plan {
 constexpr uint64_t kBlocksWanted = 4096;  // 16 a compute unit: enough loads in flight, and even ends
 
 // The entries of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
-// most what LDS has page ids for, whole pages and whole rounds of the block's wavefronts.
-uint32_t chunk_of(const KvArgs& a, uint64_t entries, uint64_t units, uint64_t wanted, uint32_t least) {
+// most `most`, whole pages and whole rounds of a block's wavefronts.
+uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t least, uint64_t most) {
   const uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
   uint64_t c = (entries + splits - 1) / splits;
   c = c < least ? least : c;
-  const uint64_t most = (uint64_t)kPagesLds * a.page;
   c = c > most ? most : c;
   return (uint32_t)up(c, 256);
 }
@@ -968,6 +982,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
   Plan p = {};
   const uint64_t row_most = (uint64_t)a.max_new * a.group;
   const uint64_t pairs = (uint64_t)a.n_seq * a.n_kv;
+  const uint64_t lds_most = (uint64_t)kPagesLds * a.page;  // entries that the few-rows kernel has page ids for
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -980,9 +995,9 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     const uint64_t all = (uint64_t)n_sel << a.page_bits;
     // a token of each sequence at least; ragged batches have fewer tokens than n_seq * max_new
     const uint64_t tokens = a.n_tok > a.n_seq ? a.n_tok : a.n_seq;
-    p.few_chunk = chunk_of(a, all, tokens * a.n_kv, kBlocksWanted, 256);
+    p.few_chunk = chunk_of(all, tokens * a.n_kv, kBlocksWanted, 256, lds_most);
     p.few_split = (uint32_t)((all + p.few_chunk - 1) / p.few_chunk);
-    p.few_cap = (uint32_t)row_most;
+    p.few_cap = 0;
     p.keys = take((size_t)a.n_tok * a.n_kv * a.max_pages * sizeof(uint32_t));
   } else {
     p.few = true;
@@ -992,20 +1007,21 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     // dimensions: 9 us against 13; 1,000 of 128: 18 against 13) and where the pairs alone fill the card (2,048
     // pairs of up to 1,000 entries: 128 us against 161).
     const bool one = (uint64_t)a.max_len * a.dim <= 65536 || (a.max_len <= 1024 && pairs >= 512);
-    p.few_chunk = one ? (uint32_t)up(a.max_len, 256) : chunk_of(a, a.max_len, pairs, kBlocksWanted, 256);
+    p.few_chunk = one ? (uint32_t)up(a.max_len, 256) : chunk_of(a.max_len, pairs, kBlocksWanted, 256, lds_most);
     p.few_split = (a.max_len + p.few_chunk - 1) / p.few_chunk;
     p.few_cap = (uint32_t)(row_most < kRowsFew ? row_most : kRowsFew);
     if (p.many) {
       const uint64_t row_tiles = (row_most + many_rows(a.dim) - 1) / many_rows(a.dim);
-      p.many_chunk = chunk_of(a, a.max_len, pairs * row_tiles, 512, 512);
+      p.many_chunk = chunk_of(a.max_len, pairs * row_tiles, 512, 512, a.max_len);
       p.many_split = (a.max_len + p.many_chunk - 1) / p.many_chunk;
     }
   }
-  if (p.few_split > 1) p.o = take((size_t)p.few_split * pairs * p.few_cap * a.dim * sizeof(float));
-  if (p.few_split > 1 || weights) p.ml = take((size_t)p.few_split * pairs * p.few_cap * sizeof(float2));
+  const size_t all_rows = (size_t)a.n_tok * a.n_q, few_part = p.few_cap ? pairs * p.few_cap : all_rows;
+  if (p.few_split > 1) p.o = take(p.few_split * few_part * a.dim * sizeof(float));
+  if (p.few_split > 1 || weights) p.ml = take(p.few_split * few_part * sizeof(float2));
   if (p.many && p.many_split > 1) {
-    p.many_o = take((size_t)p.many_split * pairs * row_most * a.dim * sizeof(float));
-    p.many_ml = take((size_t)p.many_split * pairs * row_most * sizeof(float2));
+    p.many_o = take(p.many_split * all_rows * a.dim * sizeof(float));
+    p.many_ml = take(p.many_split * all_rows * sizeof(float2));
   }
   if (weights && !p.many) {
     p.score_len = (uint32_t)up(a.max_len, 64);
@@ -1067,7 +1083,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.part_ml = (float2*)(ws + plan.many_ml);
     p.n_split = plan.many_split;
     p.chunk = plan.many_chunk;
-    p.row_cap = row_most;
+    p.row_cap = 0;
     p.rows_from = kRowsFew;
     p.rows_to = row_most;
     hipLaunchKernelGGL((kv_many_kernel<M, D>),

@@ -174,7 +174,8 @@ class Case:
                 out = sorted(range(length), key=lambda e: (keep[e], 0.0 if keep[e] else w[e], e))[:n]
                 out = sorted(out)
                 gone[i, h, :n] = out
-                fill = [e for e in range(length - n, length) if e not in set(out)]
+                goes = set(out)
+                fill = [e for e in range(length - n, length) if e not in goes]
                 src[i, h, :len(fill)] = fill
         return gone, src, new_len
 

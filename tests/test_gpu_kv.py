@@ -79,6 +79,21 @@ def test_attend_long(kv, dtype, lens, new):
     check_attend(kv, K.Case(dtype, 128, 64, 1, 8, lens, new, seed=3), max_len=max(lens))
 
 
+def test_many_tokens_over_more_pages_than_a_block_keeps(kv):
+    """17,000 entries in pages of 16: the page ids of a long chunk come in windows."""
+    check_attend(kv, K.Case("bf16", 64, 16, 1, 2, (17000, 16500), (40, 1), seed=3))
+
+
+@pytest.mark.parametrize("n_kv,seqs", [(2, 1), (2, 40)])
+def test_splits_of_loose_bounds(kv, n_kv, seqs):
+    """A page table and a bound far beyond the lengths: most pieces of the walk are empty."""
+    lens = [1 + (i * 37) % 300 for i in range(seqs)]
+    c = K.Case("fp16", 64, 32, n_kv, 2, lens, [1] * seqs, max_pages=4000, seed=1)
+    check_attend(kv, c)
+    check_attend(kv, c, max_len=100000)
+    check_blocks(kv, c, 4, 1, 1)
+
+
 @pytest.mark.parametrize("missing", [[(0, 0)], [(0, 1), (0, 2), (1, 0)], [(0, 4), (1, 0), (1, 1), (1, 2)]])
 def test_pages_that_are_not_there(kv, missing):
     """Holes at the start, inside, at the end, and a sequence without any page."""
@@ -235,6 +250,23 @@ def test_blocks_many_pages_and_ties(kv):
     check_blocks(kv, c, 33, 0, 1)
 
 
+@pytest.mark.parametrize("bound", [300, 1500, 6000, 12000, 32768])
+def test_blocks_by_the_bound_on_pages(kv, bound):
+    """The kernel that chooses goes by the bound on the lengths: each of them, on the same pages."""
+    c = K.Case("bf16", 64, 16, 1, 2, (4500, 900), (2, 1), max_pages=bound, seed=5)
+    check_blocks(kv, c, 9, 1, 2)
+
+
+def test_blocks_of_a_very_long_sequence(kv):
+    c = K.Case("fp16", 64, 16, 1, 1, (144000,), (1,), seed=6)
+    check_blocks(kv, c, 50, 2, 3)
+
+
+def test_blocks_more_than_a_block_keeps(kv):
+    """Over 1,024 chosen pages: a second piece of the walk."""
+    check_blocks(kv, K.Case("bf16", 64, 16, 1, 2, (20000, 17000), (2, 1), seed=7), 1100, 0, 1)
+
+
 def test_blocks_zero_queries_and_missing_pages(kv):
     c = K.Case("fp16", 64, 16, 2, 2, (300, 200), (1, 2), missing=[(0, 3), (0, 18), (1, 0), (1, 12)], seed=4)
     check_blocks(kv, c, 5, 1, 2)
@@ -282,6 +314,30 @@ def test_eviction_of_long_sequences(kv):
         c = K.Case("bf16", 64, 64, 1, 1, (5000, 2100, 1024), (0, 0, 0), seed=1, ties=ties)
         check_victims(kv, c, 1000, 4, 64, 5000)
         check_victims(kv, c, 4999, 4, 64, 1)
+
+
+@pytest.mark.parametrize("bound", [1000, 4096, 8000, 16000, 32768, 65536, 65552])
+def test_eviction_by_the_bound_on_lengths(kv, bound):
+    """The kernel goes by the bound on the lengths: each of them, on the same entries."""
+    for ties in (False, True):
+        c = K.Case("bf16", 64, 16, 2, 1, (900, 300, 0), (0, 0, 0), max_pages=(bound + 15) // 16, seed=2, ties=ties)
+        check_victims(kv, c, 299, 3, 40, 700)
+        check_victims(kv, c, 899, 3, 40, 2)
+        check_victims(kv, c, 298, 0, 298, 2)
+
+
+@pytest.mark.parametrize("length", [15000, 31001, 65536, 66001])
+def test_eviction_of_very_long_sequences(kv, length):
+    c = K.Case("bf16", 64, 256, 1, 1, (length, length - 7), (0, 0), seed=3)
+    check_victims(kv, c, length // 3, 4, 100, length)
+    check_victims(kv, c, length - 2, 4, 100, 3)
+
+
+def test_eviction_of_equal_weights(kv):
+    """Weights that were never added to: the lowest slots of the unprotected."""
+    c = K.Case("bf16", 64, 64, 1, 1, (20000, 3000), (0, 0), seed=3)
+    c.weight[:] = 0.0
+    check_victims(kv, c, 1000, 4, 100, 20000)
 
 
 def test_eviction_of_odd_weights(kv):
