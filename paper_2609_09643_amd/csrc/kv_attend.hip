@@ -961,7 +961,8 @@ size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 // How a call is split and where its workspace lies.
 struct Plan {
   uint32_t few_rows;       // rows of a tile of the few-rows kernel: 16 or 32
-  bool few, many;          // which kernels run
+  uint32_t few_most;       // rows of a pair up to which that kernel serves it; 0: none
+  bool many;               // whether the many-rows kernel runs, for sequences of more rows
   uint32_t few_chunk, few_split, few_cap, many_chunk, many_split, score_len;
   size_t o, ml, many_o, many_ml, scores, lse, keys, bytes;
 };
@@ -990,8 +991,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     return was;
   };
   if (n_sel) {
-    p.few = true;
-    p.few_rows = a.group > 16 ? 32 : 16;
+    p.few_rows = p.few_most = a.group > 16 ? 32 : 16;
     const uint64_t all = (uint64_t)n_sel << a.page_bits;
     // a token of each sequence at least; ragged batches have fewer tokens than n_seq * max_new
     const uint64_t tokens = a.n_tok > a.n_seq ? a.n_tok : a.n_seq;
@@ -1000,16 +1000,23 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.few_cap = 0;
     p.keys = take((size_t)a.n_tok * a.n_kv * a.max_pages * sizeof(uint32_t));
   } else {
-    p.few = true;
-    p.few_rows = row_most > 16 ? 32 : 16;
-    p.many = row_most > kRowsFew;
+    // 17 to 32 rows: two row tiles leave the few-rows kernel fewer loads under way, but it needs no second pass
+    // for the weights and ends sooner where there is little to read.  (16 sequences of 8,192 entries, 8 heads,
+    // 8 tokens of 4 query heads: 142 us against 113 on the many-rows kernel; one of them 19 against 25; 13 of
+    // 5,003, one head of 256: 24 against 52; with weights 172 against 184, at 256 dimensions 251 against 212.)
+    const bool wide = a.dim >= 128 && pairs * a.max_len * a.dim * 4 >= 160000000ull && (!weights || a.dim == 256);
+    // Up to 16 rows: of 256 dimensions the few-rows kernel has two wavefronts' registers only (the same 16
+    // sequences, one token each: 130 us against 113).
+    p.few_most = !wide ? kRowsFew : a.dim == 256 && !weights ? 0 : 16;
+    p.few_rows = row_most > 16 && !wide ? 32 : 16;
+    p.many = row_most > p.few_most;
     // One block: no second launch.  It pays where a block is done within a few tiles (777 entries of 64
-    // dimensions: 9 us against 13; 1,000 of 128: 18 against 13) and where the pairs alone fill the card (2,048
-    // pairs of up to 1,000 entries: 128 us against 161).
+    // dimensions: 9 us in one, 13 split; but 1,000 of 128: 18 in one, 13 split) and where the pairs alone fill the
+    // card (2,048 pairs of up to 1,000 entries: 128 us in one, 161 split).
     const bool one = (uint64_t)a.max_len * a.dim <= 65536 || (a.max_len <= 1024 && pairs >= 512);
     p.few_chunk = one ? (uint32_t)up(a.max_len, 256) : chunk_of(a.max_len, pairs, kBlocksWanted, 256, lds_most);
     p.few_split = (a.max_len + p.few_chunk - 1) / p.few_chunk;
-    p.few_cap = (uint32_t)(row_most < kRowsFew ? row_most : kRowsFew);
+    p.few_cap = (uint32_t)(row_most < p.few_most ? row_most : p.few_most);
     if (p.many) {
       const uint64_t row_tiles = (row_most + many_rows(a.dim) - 1) / many_rows(a.dim);
       p.many_chunk = chunk_of(a.max_len, pairs * row_tiles, 512, 512, a.max_len);
@@ -1017,8 +1024,9 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     }
   }
   const size_t all_rows = (size_t)a.n_tok * a.n_q, few_part = p.few_cap ? pairs * p.few_cap : all_rows;
+  if (p.few_most == 0) p.few_split = 0;
   if (p.few_split > 1) p.o = take(p.few_split * few_part * a.dim * sizeof(float));
-  if (p.few_split > 1 || weights) p.ml = take(p.few_split * few_part * sizeof(float2));
+  if (p.few_split > 1 || (weights && !p.many)) p.ml = take(p.few_split * few_part * sizeof(float2));
   if (p.many && p.many_split > 1) {
     p.many_o = take(p.many_split * all_rows * a.dim * sizeof(float));
     p.many_ml = take(p.many_split * all_rows * sizeof(float2));
@@ -1057,7 +1065,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
   p.chunk = plan.few_chunk;
   p.row_cap = plan.few_cap;
   p.rows_from = 0;
-  p.rows_to = plan.few_rows;
+  p.rows_to = plan.few_most;
   if (n_sel) {
     const dim3 grid(plan.few_split * a.max_new * ((a.group + plan.few_rows - 1) / plan.few_rows), a.n_kv, a.n_seq);
     if (plan.few_rows == 16) launch(kv_few_kernel<M, D, 1, true, false>, grid);
@@ -1072,7 +1080,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.score_len = plan.score_len;
     if (plan.few_rows == 16) launch(kv_few_kernel<M, D, 1, false, true>, grid);
     else launch(kv_few_kernel<M, D, 2, false, true>, grid);
-  } else {
+  } else if (plan.few_most) {
     if (plan.few_rows == 16) launch(kv_few_kernel<M, D, 1, false, false>, grid);
     else launch(kv_few_kernel<M, D, 2, false, false>, grid);
   }
@@ -1084,7 +1092,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.n_split = plan.many_split;
     p.chunk = plan.many_chunk;
     p.row_cap = 0;
-    p.rows_from = kRowsFew;
+    p.rows_from = plan.few_most;
     p.rows_to = row_most;
     hipLaunchKernelGGL((kv_many_kernel<M, D>),
                        dim3(a.n_kv * plan.many_split, (row_most + many_rows(D) - 1) / many_rows(D), a.n_seq),
