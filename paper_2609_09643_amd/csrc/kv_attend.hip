@@ -56,6 +56,9 @@ constexpr uint32_t kManyKeys = 64;
 constexpr uint32_t many_waves(uint32_t dim) { return dim <= 128 ? 8 : 4; }
 constexpr uint32_t many_rows(uint32_t dim) { return 32 * many_waves(dim); }
 
+// Bytes of scores that a few-rows block keeps in LDS and writes at its end, in one run (64 sequences of 3,300
+// to 16,384 entries, 32 query heads: 573 us, written as they come 584).
+constexpr size_t kScoresLds = 40960;
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -73,7 +76,7 @@ struct Attn {
   float* part_o;        // [..][dim], times the exponential of the maximum
   float2* part_ml;      // maximum (power of two) and sum
   float* scores;        // of the dense few-rows kernel (score_at), or null
-  uint32_t n_split, chunk, row_cap, score_len;
+  uint32_t n_split, chunk, row_cap, score_len, score_lds;
   uint32_t rows_from, rows_to;  // rows of a sequence that this launch serves: rows_from < n * group <= rows_to
 };
 
@@ -111,6 +114,9 @@ __device__ __forceinline__ void store4(typename M::t* out, const float (&x)[N]) 
 // the matrix operands, and join their maxima, sums and products in LDS at the end.  64 entries of a
 // dimension are a line of V (of 128 bytes): with 32 a wavefront, two of them fetched every line.  With
 // SPARSE a block serves one token and reads the pages of its choice instead of all.
+// 64 sequences of 9,856 entries, 8 kv heads of 128, one token each: 450 us, 5.7 TB/s (a plain read of as many
+// scattered pages of 16 KiB reaches 6.1); ragged ones of the same sum 460 to 500.  The scores for the weights
+// cost 80 us more.
 template <typename M, int D, int NT, bool SPARSE, bool SCORES>
 __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(Attn p) {
   typedef typename M::t T;
@@ -121,6 +127,7 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
   __shared__ int32_t eb[SPARSE ? kPagesLds + 4 : 1];
   __shared__ f32x4 join[(kWaves / 2) * NT * DT * 64];
   __shared__ float2 join_ml[(kWaves / 2) * NT * 64];
+  extern __shared__ f32x4 kept[];  // the chunk's scores until the end, where they fit
   const KvArgs& a = p.a;
   const uint32_t h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x, lane = tid & 63u;
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
@@ -242,7 +249,8 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
           for (int x = 0; x < 8; ++x)
             if (vpage[y] < 0 || mine[y] + x >= limit[n]) z[y][x] = -kInf;
         if (SCORES && r16 + 16u * n < rows) {
-          f32x4* to = score_at(p, s, h, (i >> 5) + y, 0, r16 + 16u * n) + g4;
+          const uint32_t at = (((i - start) >> 5) + y) * 2 * p.row_cap + r16 + 16u * n;
+          f32x4* to = (p.score_lds ? kept : score_at(p, s, h, start >> 5, 0, 0)) + 4u * at + g4;
           to[0] = f32x4{z[y][0], z[y][1], z[y][2], z[y][3]};
           to[4u * p.row_cap] = f32x4{z[y][4], z[y][5], z[y][6], z[y][7]};
         }
@@ -298,6 +306,11 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
     }
     __syncthreads();
   }
+  if (SCORES && p.score_lds && start < end) {  // everybody's scores are there: one run of memory
+    f32x4* to = score_at(p, s, h, start >> 5, 0, 0);
+    const uint32_t words = ((end - start + 63u) >> 6) * 16u * p.row_cap;
+    for (uint32_t x = tid; x < words; x += kBlock) to[x] = kept[x];
+  }
   if (wave) return;
   for (int n = 0; n < NT; ++n) {
     const uint32_t r = r16 + 16u * n;
@@ -318,7 +331,8 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
   }
 }
 
-// Joins the splits of a few- or many-rows launch: 1024 / dim rows a block, 4 dimensions a thread.
+// Joins the splits of a few- or many-rows launch: 1024 / dim rows a block, 4 dimensions a thread.  Bound by
+// latency: 16 splits are asked for at once (4 us for 16 splits of 32 rows; one after the other 11 us).
 template <typename M, int D>
 __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
   const KvArgs& a = p.a;
@@ -362,7 +376,7 @@ __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
 }
 
 // weight = decay * weight + sum of p, from the scores that the few-rows kernel left: a thread per
-// four entries.
+// four entries.  Bound by memory: 26 us for 5 million entries of 4 rows each (120 MB, 4.6 TB/s).
 __global__ __launch_bounds__(kBlock) void kv_weight_few_kernel(Attn p, float decay) {
   __shared__ float base[kRowsFew];
   const KvArgs& a = p.a;
@@ -458,6 +472,9 @@ __device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(sc
 // much, by the exponentials (a quarter of the rate) and the additions and roundings beside them, so the
 // two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
 // the second product of the group before and the first product of the group behind.
+// 4 sequences of up to 2,000 tokens over up to 12,001 entries, 32 query and 8 kv heads of 128 (928 GFLOP seen):
+// 860 us, 1.08 PFLOP/s; a large library product reaches 1.38.  Its matrix cores are busy 51 % of the time, its
+// vector units 39 %.
 template <typename M, int D>
 __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {
   typedef typename M::t T;
@@ -775,7 +792,8 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
 // weight = decay * weight + the sum of p over a sequence's rows, which another product of the keys with
 // the queries gives, the entries in the lanes now and the rows in their registers: 64 entries a wavefront
 // with their keys in registers, 64 rows at a time from double-buffered LDS.  As above, the exponentials of
-// 32 rows run beside the products of the next 32; the two take about the same time.
+// 32 rows run beside the products of the next 32; the two take about the same time.  620 us for the sequences
+// named there (464 GFLOP; matrix cores 44 % busy, vector units 62 %).
 constexpr uint32_t kWeightKeys = 256, kWeightRows = 64;
 
 template <typename M, int D>
@@ -967,7 +985,9 @@ struct Plan {
   size_t o, ml, many_o, many_ml, scores, lse, keys, bytes;
 };
 
-constexpr uint64_t kBlocksWanted = 4096;  // 16 a compute unit: enough loads in flight, and even ends
+// Blocks of a few-rows launch, 16 a compute unit: enough loads under way and even ends (64 ragged sequences as
+// above: 613 us with 2,048, 583 with 4,096, 600 with 8,192).
+constexpr uint64_t kBlocksWanted = 4096;
 
 // The entries of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
 // most `most`, whole pages and whole rounds of a block's wavefronts.
@@ -1019,6 +1039,8 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.few_cap = (uint32_t)(row_most < p.few_most ? row_most : p.few_most);
     if (p.many) {
       const uint64_t row_tiles = (row_most + many_rows(a.dim) - 1) / many_rows(a.dim);
+      // 512 blocks, two a compute unit (64 tokens over 60,000 entries: 110 us, unsplit 1,558; 4 sequences' 200
+      // tokens over 20,000: 337 and 540)
       p.many_chunk = chunk_of(a.max_len, pairs * row_tiles, 512, 512, a.max_len);
       p.many_split = (a.max_len + p.many_chunk - 1) / p.many_chunk;
     }
@@ -1078,8 +1100,13 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
   if (scores) {
     p.scores = (float*)(ws + plan.scores);
     p.score_len = plan.score_len;
-    if (plan.few_rows == 16) launch(kv_few_kernel<M, D, 1, false, true>, grid);
-    else launch(kv_few_kernel<M, D, 2, false, true>, grid);
+    const size_t bytes = (size_t)plan.few_chunk * plan.few_cap * sizeof(float);
+    p.score_lds = bytes <= kScoresLds;
+    const auto scored = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(kBlock), p.score_lds ? bytes : 0, st, p);
+    };
+    if (plan.few_rows == 16) scored(kv_few_kernel<M, D, 1, false, true>);
+    else scored(kv_few_kernel<M, D, 2, false, true>);
   } else if (plan.few_most) {
     if (plan.few_rows == 16) launch(kv_few_kernel<M, D, 1, false, false>, grid);
     else launch(kv_few_kernel<M, D, 2, false, false>, grid);

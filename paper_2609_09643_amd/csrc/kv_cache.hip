@@ -90,6 +90,9 @@ __device__ void write_box(const KvArgs& a, int32_t page, uint32_t h, const Sides
 // where the pool has boxes, through the box's sides on the way, together with the page's older rows.
 // Values change their order: 64 slots of the page are put together in LDS, two slots to a word, and
 // leave in 16-byte runs of slots; up to kDirect new rows (a decode step) go straight to their places.
+// Bound by memory: 16 sequences' turns of up to 2,000 tokens, 8 heads of 128 (158 MB): 42 us, 3.8 TB/s; a step of
+// 64 tokens 5.8 us, most of it latency.  A step of 4 tokens each takes 10.3 us direct, 10.9 through LDS; of
+// 8 12.5 and 10.5.
 constexpr int32_t kDirect = 4;
 
 template <typename T, int D>
@@ -331,9 +334,13 @@ __device__ __forceinline__ Bits<PER> pick_chosen(const uint32_t (&key)[PER], Cut
 
 // ------------------------------------------------------------------ victims
 
-constexpr uint32_t kFewVictims = 4;  // up to which rounds of a minimum beat the digits' histograms
+// Up to so many victims, rounds of a minimum beat the digits' histograms (one of 20,000 entries: 16 us, 38 with
+// histograms; one of 4,097 in 512 pairs: 14 and 20).
+constexpr uint32_t kFewVictims = 4;
 
-// One block per (kv head, sequence) of up to BLOCK * PER entries: weights and positions are read once.
+// One block per (kv head, sequence) of up to BLOCK * PER entries: weights and positions are read once into
+// registers (twice of more than 32 a thread).  Bound by latency, that of its chain of loads and barriers: 8
+// sequences of up to 32,768 entries and 8 heads (64 blocks) down to 8,192: 40 us for 25 MB.
 template <int BLOCK, int PER>
 __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
                                                            uint32_t recent, uint32_t max_evict,
@@ -458,7 +465,8 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvA
   for (uint32_t i = moved + tid; i < max_evict; i += BLOCK) src[row + i] = -1;
 }
 
-// Longer sequences than a block's registers hold are read again in every pass.
+// Longer sequences than a block's registers hold are read again in every pass (8 of up to 66,000 entries:
+// 390 us; of 60,000 in registers 87).
 constexpr uint32_t kSelBlock = 1024;
 
 // Inclusive sum over the block of a word per thread; `total` is the block's.
@@ -646,7 +654,10 @@ __global__ __launch_bounds__(kBlock) void kv_compact_few_kernel(KvArgs a, uint32
 }
 
 // Many moves: 64 of a block, whose places lie close together, with a lane per move for the values, so
-// that a load takes its 64 slots of a dimension from a few lines.
+// that a load takes its 64 slots of a dimension from a few lines (a lane per dimension took 64 lines for 64
+// values: 312 us for 8 sequences of up to 32,768 entries down to 8,192, 8 heads of 128; now 190).  Bound by the
+// lines that the values touch: a dimension's 64 slots are one, and most lines behind the new end and
+// most of those before it are touched, 0.7 GB in all where the moved entries are 0.37.
 template <int D>
 __global__ __launch_bounds__(kBlock) void kv_compact_kernel(KvArgs a, uint32_t max_evict,
                                                             const int32_t* victims, const int32_t* src,
@@ -720,7 +731,8 @@ constexpr uint32_t kScorePages = 64;  // of a block, 16 a wavefront
 //   sum over heads and dimensions of max(qi lower, qi upper)
 //     = sum over dimensions of (sum over heads of min(qi, 0)) lower + (sum over heads of max(qi, 0)) upper,
 // one product with the box's bytes for all heads of the group.  The summed query has up to 15 bits: two
-// 7-bit halves, so that the products are byte dot products.  Bound by the boxes' bytes.
+// 7-bit halves, so that the products are byte dot products.  Bound by latency and the boxes' bytes: 2,047 pages,
+// 8 heads of 128: 5.4 us; 24 sequences of up to 512 pages and 2 tokens: 12.5 us (32 MB of boxes).
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, uint32_t first, uint32_t last,
                                                           uint32_t* keys) {
@@ -791,6 +803,7 @@ __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, u
   keys[(t * a.n_kv + h) * a.max_pages + (uint32_t)mine] = key;
 }
 
+// The n_sel pages of smallest key, one block per (token, kv head).  Bound by latency: 8.5 us for 64 of 2,047.
 template <int BLOCK, int PER>
 __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_choose_kernel(KvArgs a, uint32_t n_sel, const uint32_t* keys,
                                                           int32_t* sel) {
@@ -842,8 +855,8 @@ hipError_t with_type(const KvArgs& a, F f) {
   });
 }
 
-// The smallest block whose registers hold `n` keys: fewer wavefronts meet at fewer barriers, and more
-// blocks fit a compute unit.
+// The smallest block whose registers hold `n` keys, of 1,024 threads rather than more keys a thread (2,047
+// keys: 8.5 us with 1,024 x 4, 12.2 with 256 x 16).
 template <typename F>
 bool with_pick(uint32_t n, F f) {
   if (n <= 1024) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
