@@ -435,17 +435,10 @@ __device__ __forceinline__ uint32_t swap23(uint32_t x) {
   return (x & ~12u) | ((x & 4u) << 1) | ((x & 8u) >> 1);
 }
 
-// Where a row of `CH` 16-byte pieces keeps piece c: xored with the row, so that 16 rows' pieces c, which
-// a read takes at once, lie in different banks (64 banks hold two rows of 8 pieces).
-template <uint32_t CH>
-__device__ __forceinline__ uint32_t spread(uint32_t row) {
-  return CH == 8 ? (row >> 1) & 7u : row & 15u;
-}
-
-// The same for rows that keep only the offsets' lane-dependent part small: a kibibyte (64 pieces, what a
-// wavefront loads at once) takes kRun bytes, the 64 more bytes turning the next one's banks by a quarter, and
-// inside it a row's pieces are xored with two bits of the row.  16 rows' pieces c lie in different banks, and the
-// address of piece c is the lane's for c mod 4 and a constant.
+// Where rows of CH 16-byte pieces lie in LDS, so that 16 rows' pieces c, which a read takes at once, lie in
+// different banks (64 of them: 256 bytes): a kibibyte (64 pieces, what a wavefront loads at once) takes kRun
+// bytes, the 64 more turning the next one's banks by a quarter, and inside it a row's pieces are xored with two
+// bits of the row.  The address of piece c is then the lane's for c mod 4 and a constant.
 constexpr uint32_t kRun = 1024 + 64;
 template <uint32_t CH>
 __device__ __forceinline__ uint32_t turn(uint32_t row) {
@@ -469,7 +462,7 @@ __device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(sc
 
 // Attention of 128 or 256 rows over a chunk of entries, 32 rows a wavefront, 64 entries at a time from
 // double-buffered LDS: a turn's new tokens over their session.  Bound by the matrix cores and, nearly as
-// much, by the exponentials (a quarter of the rate) and the additions and roundings beside them, so the
+// much, by the exponentials (at half the rate of an addition) and the additions and roundings beside them, so the
 // two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
 // the second product of the group before and the first product of the group behind.
 // 4 sequences of up to 2,000 tokens over up to 12,001 entries, 32 query and 8 kv heads of 128 (928 GFLOP seen):

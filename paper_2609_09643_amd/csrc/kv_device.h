@@ -42,7 +42,7 @@ struct KvSeq {
   const int32_t* pages;
 };
 
-__device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, uint32_t s) {
+__host__ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, uint32_t s) {
   KvSeq q;
   const int32_t l = a.len[s];
   q.len = l < 0 ? 0 : (uint32_t)l > a.max_len ? (int32_t)a.max_len : l;
@@ -66,16 +66,16 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, uint32_t s) {
 __device__ __forceinline__ uint32_t spread_piece(uint32_t x, uint32_t n) { return (x + blockIdx.y + blockIdx.z) % n; }
 
 // The page of ordinal `o` (below max_pages), or -1 where there is none.
-__device__ __forceinline__ int32_t kv_page(const KvArgs& a, const KvSeq& q, int32_t o) {
+__host__ __device__ __forceinline__ int32_t kv_page(const KvArgs& a, const KvSeq& q, int32_t o) {
   const int32_t p = q.pages[o];
   return (uint32_t)p < a.n_pages ? p : -1;
 }
 // First element of a page's keys (values) of kv head h.
-__device__ __forceinline__ size_t kv_base(const KvArgs& a, int32_t page, uint32_t h) {
+__host__ __device__ __forceinline__ size_t kv_base(const KvArgs& a, int32_t page, uint32_t h) {
   return ((size_t)page * a.n_kv + h) * a.page * a.dim;
 }
 // First entry of a page's per-entry words (weights, positions) of kv head h.
-__device__ __forceinline__ size_t kv_word(const KvArgs& a, int32_t page, uint32_t h) {
+__host__ __device__ __forceinline__ size_t kv_word(const KvArgs& a, int32_t page, uint32_t h) {
   return ((size_t)page * a.n_kv + h) * a.page;
 }
 

@@ -180,6 +180,42 @@ def test_shared_pages(kv):
     assert (out[0] == out[1]).all()
 
 
+def test_pages_past_32_bits(kv):
+    """Pages whose elements' offsets pass 2^32: every operator as on the same pages of a small pool."""
+    import torch
+    c = K.Case("bf16", 128, 64, 8, 2, (300, 150), (2, 1), seed=12)
+    small, seqs = K.device(c)
+    n_pages = (1 << 32) // (8 * 64 * 128) + 100
+    shape = (n_pages, 8, 64, 128)
+    big = kv.Pool(torch.empty(shape, dtype=torch.bfloat16, device="cuda"),
+                  torch.empty((n_pages, 8, 128, 64), dtype=torch.bfloat16, device="cuda"),
+                  torch.empty(shape[:3], dtype=torch.float32, device="cuda"),
+                  torch.empty(shape[:3], dtype=torch.int32, device="cuda"),
+                  torch.empty((n_pages, 8, 2, 128), dtype=torch.int8, device="cuda"),
+                  torch.empty((n_pages, 8), dtype=torch.float32, device="cuda"))
+    at = torch.arange(n_pages - c.n_pages, n_pages, device="cuda")   # all beyond 2^32 elements
+    names = ("k", "v", "weight", "pos", "box", "box_scale")
+    for name in names:
+        getattr(big, name)[at] = getattr(small, name)
+    pages = torch.where(seqs.pages >= 0, seqs.pages + (n_pages - c.n_pages), -1).to(torch.int32)
+    far = kv.Seqs(pages, seqs.length, seqs.tok, n_tok=c.n_tok, max_new=2)
+    q, pos = K.rows(c.q, "bf16"), torch.arange(c.n_tok, dtype=torch.int32, device="cuda")
+    new = K.rows(c.new_k, "bf16"), K.rows(c.new_v, "bf16")
+    for a, b in ((small, seqs), (big, far)):
+        kv.append(a, b, *new, pos)
+    assert torch.equal(kv.attend(small, seqs, q, decay=0.5), kv.attend(big, far, q, decay=0.5))
+    for x, y in zip(kv.attend_blocks(small, seqs, q, 3), kv.attend_blocks(big, far, q, 3)):
+        assert torch.equal(x, y)
+    gone = kv.victims(small, seqs, 120, 4, 16, 200)
+    for x, y in zip(gone, kv.victims(big, far, 120, 4, 16, 200)):
+        assert torch.equal(x, y)
+    kv.compact(small, seqs, *gone)
+    kv.compact(big, far, *gone)
+    for name in names:
+        x, y = getattr(small, name), getattr(big, name)[at]
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), name
+
+
 # ------------------------------------------------------------------ append
 
 @pytest.mark.parametrize("dtype,dim,page,n_kv,lens,new", [
