@@ -676,6 +676,9 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) read(u);
+    // Ahead of the SIMD's other wavefront while there are products, which then does what has none beside it
+    // (two prompts of 8,000 tokens: 1,040 us without, 1,007 with).
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       __builtin_amdgcn_sched_barrier(0);
@@ -689,6 +692,7 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
         if (x) rest(x - 1);  // the result of an exponential is not there at once
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     rest(15);
     l0 += l1;
     asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l0));
