@@ -77,6 +77,8 @@ struct Attn {
   float2* part_ml;      // maximum (power of two) and sum
   float* scores;        // of the dense few-rows kernel (score_at), or null
   uint32_t n_split, chunk, row_cap, score_len, score_lds;
+  float* part_w;        // weights' sums of a split of the rows, [w_split][n_seq][n_kv][w_len]
+  uint32_t w_split, w_rows, w_len;
   uint32_t rows_from, rows_to;  // rows of a sequence that this launch serves: rows_from < n * group <= rows_to
 };
 
@@ -806,7 +808,8 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kerne
   const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
   const KvSeq q = kv_seq(a, s);
   const uint32_t rows = (uint32_t)q.n * a.group;
-  const int32_t first = (int32_t)(spread_piece(blockIdx.x, gridDim.x) * kWeightKeys), mine = first + (int32_t)(64u * wave);
+  const uint32_t split = blockIdx.x % p.w_split, piece_of = spread_piece(blockIdx.x / p.w_split, gridDim.x / p.w_split);
+  const int32_t first = (int32_t)(piece_of * kWeightKeys), mine = first + (int32_t)(64u * wave);
   if (rows == 0 || first >= q.len) return;
   const int32_t old = q.len - q.n;
   const float scale = magnitude(p.scale2);
@@ -821,11 +824,14 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kerne
 #pragma unroll
     for (int k = 0; k < KS; ++k) kf[y][k] = signed_row(*(const v8*)(key + 16 * k + 8 * half), negate);
   }
-  // rows of tokens before entry `first` see nothing here
-  const uint32_t from = first > old ? ((uint32_t)(first - old) * a.group) & ~(kWeightRows - 1u) : 0u;
-  const int32_t tiles = from < rows ? (int32_t)((rows - from + kWeightRows - 1u) / kWeightRows) : 0;
+  // the split's rows; those of tokens before entry `first` see nothing here
+  uint32_t from = first > old ? ((uint32_t)(first - old) * a.group) & ~(kWeightRows - 1u) : 0u;
+  from = from > split * p.w_rows ? from : split * p.w_rows;
+  const uint32_t to = rows < (split + 1u) * p.w_rows ? rows : (split + 1u) * p.w_rows;
+  const int32_t tiles = from < to ? (int32_t)((to - from + kWeightRows - 1u) / kWeightRows) : 0;
   // the first tile with a row that sees an entry of the wavefront
-  const int32_t begin = mine > old ? (int32_t)(((uint32_t)(mine - old) * a.group - from) / kWeightRows) : 0;
+  const uint32_t seen_from = mine > old ? (uint32_t)(mine - old) * a.group : 0u;
+  const int32_t begin = seen_from > from ? (int32_t)((seen_from - from) / kWeightRows) : 0;
   // token and head of the lane's rows of the next tile, moved on without dividing
   const uint32_t dj = kWeightRows / a.group, dg = kWeightRows % a.group;
   uint32_t rj[NQ], rg[NQ], part[NQ], bj = 0, bg = 0;
@@ -964,9 +970,29 @@ __global__ __launch_bounds__(kBlock, D <= 128 ? 2 : 1) void kv_weight_many_kerne
   for (int y = 0; y < 2; ++y) {
     sum[y] += __shfl_xor(sum[y], 32);
     if (page[y] < 0 || half) continue;
-    float* w = a.weight + kv_word(a, page[y], h) + ((uint32_t)(mine + 32 * y + (int32_t)c32) & (a.page - 1u));
+    const uint32_t e = (uint32_t)mine + 32u * y + c32;
+    if (p.w_split > 1) {
+      p.part_w[(((size_t)split * a.n_seq + s) * a.n_kv + h) * p.w_len + e] = sum[y];
+      continue;
+    }
+    float* w = a.weight + kv_word(a, page[y], h) + (e & (a.page - 1u));
     *w = fmaf(decay, *w, sum[y]);
   }
+}
+
+// weight = decay * weight + the sums of the splits of the rows, in their order.
+__global__ __launch_bounds__(kBlock) void kv_weight_join_kernel(Attn p, float decay) {
+  const KvArgs& a = p.a;
+  const uint32_t h = blockIdx.y, s = blockIdx.z, e = blockIdx.x * kBlock + threadIdx.x;
+  const KvSeq q = kv_seq(a, s);
+  if (q.n <= 0 || e >= (uint32_t)q.len) return;
+  const int32_t page = kv_page(a, q, (int32_t)(e >> a.page_bits));
+  if (page < 0) return;
+  float sum = 0.0f;
+#pragma unroll 8
+  for (uint32_t i = 0; i < p.w_split; ++i) sum += p.part_w[(((size_t)i * a.n_seq + s) * a.n_kv + h) * p.w_len + e];
+  float* w = a.weight + kv_word(a, page, h) + (e & (a.page - 1u));
+  *w = fmaf(decay, *w, sum);
 }
 
 // ------------------------------------------------------------------ plans
@@ -979,19 +1005,26 @@ struct Plan {
   uint32_t few_most;       // rows of a pair up to which that kernel serves it; 0: none
   bool many;               // whether the many-rows kernel runs, for sequences of more rows
   uint32_t few_chunk, few_split, few_cap, many_chunk, many_split, score_len;
-  size_t o, ml, many_o, many_ml, scores, lse, keys, bytes;
+  uint32_t w_split, w_rows, w_len;
+  size_t o, ml, many_o, many_ml, scores, lse, part_w, keys, bytes;
 };
 
 // Blocks of a few-rows launch, 16 a compute unit: enough loads under way and even ends (64 ragged sequences as
 // above: 613 us with 2,048, 583 with 4,096, 600 with 8,192).
 constexpr uint64_t kBlocksWanted = 4096;
 
-// The entries of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
+// Blocks of the many-rows weights: two a compute unit, the rows split where the entries alone give fewer (2,000
+// tokens over themselves, 32 query and 8 kv heads: 106 us without weights, 156 with, 289 with unsplit rows).
+constexpr uint64_t kWeightBlocks = 512;
+
+// The entries (or rows) of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
 // most `most`, whole pages and whole rounds of a block's wavefronts.
 uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t least, uint64_t most) {
-  const uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
+  uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
+  // none is shorter than `least` (23 sequences' 136 tokens over 514, 256 dimensions: 73 us, split 512 + 2 188)
+  const uint64_t fit = entries / least > 1 ? entries / least : 1;
+  splits = splits < fit ? splits : fit;
   uint64_t c = (entries + splits - 1) / splits;
-  c = c < least ? least : c;
   c = c > most ? most : c;
   return (uint32_t)up(c, 256);
 }
@@ -1054,7 +1087,13 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.score_len = (uint32_t)up(a.max_len, 64);
     p.scores = take(pairs * p.few_cap * p.score_len * sizeof(float));
   }
-  if (weights && p.many) p.lse = take((size_t)a.n_tok * a.n_q * sizeof(float));
+  if (weights && p.many) {
+    p.lse = take((size_t)a.n_tok * a.n_q * sizeof(float));
+    p.w_len = (uint32_t)up(a.max_len, kWeightKeys);
+    p.w_rows = chunk_of(row_most, pairs * (p.w_len / kWeightKeys), kWeightBlocks, 256, row_most);
+    p.w_split = (uint32_t)((row_most + p.w_rows - 1) / p.w_rows);
+    if (p.w_split > 1) p.part_w = take(p.w_split * pairs * p.w_len * sizeof(float));
+  }
   p.bytes = at;
   return p;
 }
@@ -1122,8 +1161,14 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
                        dim3(a.n_kv * plan.many_split, (row_most + many_rows(D) - 1) / many_rows(D), a.n_seq),
                        dim3(64 * many_waves(D)), 0, st, p);
     if (plan.many_split > 1) join(row_most);
-    if (weights) launch(kv_weight_many_kernel<M, D>, dim3((a.max_len + kWeightKeys - 1) / kWeightKeys, a.n_kv, a.n_seq),
-                        decay);
+    if (weights) {
+      p.part_w = (float*)(ws + plan.part_w);
+      p.w_split = plan.w_split;
+      p.w_rows = plan.w_rows;
+      p.w_len = plan.w_len;
+      launch(kv_weight_many_kernel<M, D>, dim3(plan.w_len / kWeightKeys * plan.w_split, a.n_kv, a.n_seq), decay);
+      if (plan.w_split > 1) launch(kv_weight_join_kernel, dim3((a.max_len + kBlock - 1) / kBlock, a.n_kv, a.n_seq), decay);
+    }
   }
   return hipGetLastError();
 }

@@ -74,6 +74,14 @@ def test_attend_many_tokens(kv, dtype, dim, page, n_kv, group, lens, new):
     check_attend(kv, K.Case(dtype, dim, page, n_kv, group, lens, new, seed=7))
 
 
+@pytest.mark.parametrize("dtype,dim,page,group", [("bf16", 128, 16, 4), ("fp16", 64, 64, 7), ("bf16", 256, 32, 3)])
+@pytest.mark.parametrize("lens,new", [((600,), (600,)), ((700, 30, 260, 0), (300, 1, 257, 2)), ((90,), (700,))])
+def test_weights_of_split_rows(kv, dtype, dim, page, group, lens, new):
+    """So few blocks of entries that their rows are split: some splits see nothing, some sequences have one row,
+    or tokens that see nothing, or a page that is not there."""
+    check_attend(kv, K.Case(dtype, dim, page, 1, group, lens, new, missing=[(0, 1)], seed=dim), decay=0.9)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("lens,new", [((5000, 3), (1, 1)), ((4099, 700), (4, 2)), ((2500,), (40,))])
 def test_attend_long(kv, dtype, lens, new):
