@@ -343,8 +343,9 @@ __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
   const uint32_t rows = (uint32_t)q.n * a.group, r = blockIdx.x * (4 * kBlock / D) + threadIdx.x / (D / 4);
   if (r >= rows || (!p.sel && (rows <= p.rows_from || rows > p.rows_to))) return;
   const uint32_t d = 4 * (threadIdx.x % (D / 4));
-  const uint32_t all = p.sel ? p.n_sel << a.page_bits : (uint32_t)q.len;
-  const uint32_t used = all ? (all + p.chunk - 1) / p.chunk : 1u;
+  const int32_t limit = q.len - q.n + (int32_t)(r / a.group) + 1;  // splits behind it may not be written
+  const uint32_t all = p.sel ? p.n_sel << a.page_bits : limit > 0 ? (uint32_t)limit : 0u;
+  const uint32_t used = (all + p.chunk - 1) / p.chunk;
   float m = -kInf, l = 0.0f;
   f32x4 o = (f32x4)0.0f;
   constexpr uint32_t B = 16;  // splits' loads in flight
@@ -352,11 +353,12 @@ __global__ __launch_bounds__(kBlock) void kv_join_kernel(Attn p) {
     float2 y[B];
     f32x4 x[B];
     for (uint32_t i = 0; i < B; ++i) {
-      const bool is = i0 + i < used;
-      const size_t part = part_row(p, is ? i0 + i : i0, s, h, q.t0, r);
+      y[i] = make_float2(-kInf, 0.0f);
+      x[i] = (f32x4)0.0f;
+      if (i0 + i >= used) continue;
+      const size_t part = part_row(p, i0 + i, s, h, q.t0, r);
       y[i] = p.part_ml[part];
       x[i] = *(const f32x4*)(p.part_o + part * D + d);
-      if (!is) y[i] = make_float2(-kInf, 0.0f);
     }
     float next = m;
     for (uint32_t i = 0; i < B; ++i) next = fmaxf(next, y[i].x);
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
   const int32_t block_end = old + token((tile + 1u) * ROWS - 1u) + 1;
   const uint32_t w0 = tile * ROWS + 32u * wave;
   const int32_t start = (int32_t)(split * p.chunk);
-  if (start >= q.len && split) return;
+  if (split && start >= block_end) return;  // the join knows
   int32_t end = block_end < q.len ? block_end : q.len;
   if (end > 0 && (uint32_t)end > (uint32_t)start + p.chunk) end = start + (int32_t)p.chunk;
   const int32_t tiles = end > start ? (end - start + 63) >> 6 : 0;
@@ -1029,6 +1031,44 @@ uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t le
   return (uint32_t)up(c, 256);
 }
 
+// The entries of a split of the many-rows kernel, a block of which fills a compute unit.  A block takes the time of
+// its split's tiles, of 3 more to begin and, where rows are split, of 7 to write and read what is joined, and the
+// join's launch that of 2.  One sequence's blocks are alike and run in rounds of 256; of more sequences, whose
+// lengths differ, the blocks' sum counts, three quarters of what the longest would give, and half of the longest
+// block for the end, and the longest at least.  (46 sequences' up to 137 tokens over 6,000 to 29,296 entries, 2
+// heads of 3: 374 us, by rounds 573; 2,000 tokens over themselves, 32
+// query and 8 kv heads: 65 us unsplit, 105 in two; 512 tokens over 20,000: 178 in 4, 192 in 8, 225 in 16; 64 over
+// 60,000: 93 in 32, 107 in 64; 200 of 4 sequences over 20,000: 320 in 2, 331 in 4.)
+uint32_t many_chunk_of(const KvArgs& a) {
+  constexpr uint64_t UNITS = 256;
+  const uint64_t rows = many_rows(a.dim), one = ((uint64_t)a.max_new * a.group + rows - 1) / rows;
+  // ragged batches have fewer tokens than n_seq * max_new
+  const uint64_t by_seq = one * a.n_seq, by_tok = (uint64_t)a.n_tok * a.group / rows + a.n_seq;
+  const uint64_t blocks = (by_seq < by_tok ? by_seq : by_tok) * a.n_kv;
+  const uint64_t whole = a.page > kManyKeys ? a.page : kManyKeys, least = 2 * kManyKeys;
+  uint64_t chunk = up(a.max_len, whole);
+  const auto cost_of = [&](uint64_t n, uint64_t tiles) {  // of n blocks, times 4
+    const uint64_t rounds = 4 * ((n + UNITS - 1) / UNITS) * tiles, sum = 3 * n * tiles / UNITS + 2 * tiles;
+    return a.n_seq == 1 ? rounds : sum > 4 * tiles ? sum : 4 * tiles;
+  };
+  uint64_t best = cost_of(blocks, chunk / kManyKeys + 3);
+  // two rounds even out by themselves: lengths differ, and the longest blocks come first
+  for (uint64_t rounds = 1; rounds <= 8 && blocks < 2 * UNITS; ++rounds) {
+    uint64_t splits = UNITS * rounds / blocks;
+    splits = splits * least > a.max_len ? a.max_len / least : splits;
+    if (splits < 2) continue;
+    const uint64_t c = up((a.max_len + splits - 1) / splits, whole);
+    splits = (a.max_len + c - 1) / c;
+    if (splits < 2) continue;
+    const uint64_t cost = cost_of(blocks * splits, c / kManyKeys + 10) + 8;
+    if (cost < best) {
+      best = cost;
+      chunk = c;
+    }
+  }
+  return (uint32_t)chunk;
+}
+
 Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
   Plan p = {};
   const uint64_t row_most = (uint64_t)a.max_new * a.group;
@@ -1068,10 +1108,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.few_split = (a.max_len + p.few_chunk - 1) / p.few_chunk;
     p.few_cap = (uint32_t)(row_most < p.few_most ? row_most : p.few_most);
     if (p.many) {
-      const uint64_t row_tiles = (row_most + many_rows(a.dim) - 1) / many_rows(a.dim);
-      // 512 blocks, two a compute unit (64 tokens over 60,000 entries: 110 us, unsplit 1,558; 4 sequences' 200
-      // tokens over 20,000: 337 and 540)
-      p.many_chunk = chunk_of(a.max_len, pairs * row_tiles, 512, 512, a.max_len);
+      p.many_chunk = many_chunk_of(a);
       p.many_split = (a.max_len + p.many_chunk - 1) / p.many_chunk;
     }
   }
