@@ -1017,18 +1017,19 @@ constexpr uint64_t kBlocksWanted = 4096;
 
 // Blocks of the many-rows weights: two a compute unit, the rows split where the entries alone give fewer (2,000
 // tokens over themselves, 32 query and 8 kv heads: 106 us without weights, 156 with, 289 with unsplit rows).
-constexpr uint64_t kWeightBlocks = 512;
+constexpr uint64_t kWeightBlocks = 512, kWeightLeast = 128;
 
 // The entries (or rows) of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
 // most `most`, whole pages and whole rounds of a block's wavefronts.
-uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t least, uint64_t most) {
+uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t least, uint64_t most,
+                  uint32_t whole = 256) {
   uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
   // none is shorter than `least` (23 sequences' 136 tokens over 514, 256 dimensions: 73 us, split 512 + 2 188)
   const uint64_t fit = entries / least > 1 ? entries / least : 1;
   splits = splits < fit ? splits : fit;
   uint64_t c = (entries + splits - 1) / splits;
   c = c > most ? most : c;
-  return (uint32_t)up(c, 256);
+  return (uint32_t)up(c, whole);
 }
 
 // The entries of a split of the many-rows kernel, a block of which fills a compute unit.  A block takes the time of
@@ -1100,6 +1101,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.few_most = !wide ? kRowsFew : a.dim == 256 && !weights ? 0 : 16;
     p.few_rows = row_most > 16 && !wide ? 32 : 16;
     p.many = row_most > p.few_most;
+    if (p.many && a.n_seq == 1) p.few_most = 0;  // nobody else may have few: no launches for them
     // One block: no second launch.  It pays where a block is done within a few tiles (777 entries of 64
     // dimensions: 9 us in one, 13 split; but 1,000 of 128: 18 in one, 13 split) and where the pairs alone fill the
     // card (2,048 pairs of up to 1,000 entries: 128 us in one, 161 split).
@@ -1127,7 +1129,7 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
   if (weights && p.many) {
     p.lse = take((size_t)a.n_tok * a.n_q * sizeof(float));
     p.w_len = (uint32_t)up(a.max_len, kWeightKeys);
-    p.w_rows = chunk_of(row_most, pairs * (p.w_len / kWeightKeys), kWeightBlocks, 256, row_most);
+    p.w_rows = chunk_of(row_most, pairs * (p.w_len / kWeightKeys), kWeightBlocks, kWeightLeast, row_most, kWeightRows);
     p.w_split = (uint32_t)((row_most + p.w_rows - 1) / p.w_rows);
     if (p.w_split > 1) p.part_w = take(p.w_split * pairs * p.w_len * sizeof(float));
   }
