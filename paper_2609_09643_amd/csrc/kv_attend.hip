@@ -1020,14 +1020,12 @@ constexpr uint64_t kBlocksWanted = 4096;
 constexpr uint64_t kWeightBlocks = 512, kWeightLeast = 128;
 
 // The entries (or rows) of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
-// most `most`, whole pages and whole rounds of a block's wavefronts.
+// most `most`, a multiple of `whole` (whole pages and whole rounds of a block's wavefronts).
 uint32_t chunk_of(uint64_t entries, uint64_t units, uint64_t wanted, uint64_t least, uint64_t most,
                   uint32_t whole = 256) {
-  uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
-  // none is shorter than `least` (23 sequences' 136 tokens over 514, 256 dimensions: 73 us, split 512 + 2 188)
-  const uint64_t fit = entries / least > 1 ? entries / least : 1;
-  splits = splits < fit ? splits : fit;
+  const uint64_t splits = units >= wanted ? 1 : (wanted + units - 1) / units;
   uint64_t c = (entries + splits - 1) / splits;
+  c = c < least ? least : c;
   c = c > most ? most : c;
   return (uint32_t)up(c, whole);
 }
