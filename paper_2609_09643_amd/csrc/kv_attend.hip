@@ -470,8 +470,8 @@ __device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(sc
 // two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
 // the second product of the group before and the first product of the group behind.
 // 4 sequences of up to 2,000 tokens over up to 12,001 entries, 32 query and 8 kv heads of 128 (928 GFLOP seen):
-// 860 us, 1.08 PFLOP/s; a large library product reaches 1.38.  Its matrix cores are busy 51 % of the time, its
-// vector units 39 %.
+// 890 us, 1.04 PFLOP/s; a large library product reaches 1.38.  Its matrix cores are busy 54 % of the time, its
+// vector units 41 %.  Four tiles in LDS in place of two, their loads awaited by number, took 2 to 5 % longer.
 template <typename M, int D>
 __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {
   typedef typename M::t T;
@@ -793,7 +793,7 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
 // weight = decay * weight + the sum of p over a sequence's rows, which another product of the keys with
 // the queries gives, the entries in the lanes now and the rows in their registers: 64 entries a wavefront
 // with their keys in registers, 64 rows at a time from double-buffered LDS.  As above, the exponentials of
-// 32 rows run beside the products of the next 32; the two take about the same time.  620 us for the sequences
+// 32 rows run beside the products of the next 32; the two take about the same time.  565 us for the sequences
 // named there (464 GFLOP; matrix cores 44 % busy, vector units 62 %).
 constexpr uint32_t kWeightKeys = 256, kWeightRows = 64;
 
@@ -1015,8 +1015,8 @@ struct Plan {
 // above: 613 us with 2,048, 583 with 4,096, 600 with 8,192).
 constexpr uint64_t kBlocksWanted = 4096;
 
-// Blocks of the many-rows weights: two a compute unit, the rows split where the entries alone give fewer (2,000
-// tokens over themselves, 32 query and 8 kv heads: 106 us without weights, 156 with, 289 with unsplit rows).
+// Blocks of the many-rows weights: two a compute unit, the rows split, at least 128 of them each, where the entries
+// alone give fewer (2,000 tokens over themselves, 32 query and 8 kv heads: 50 us, with unsplit rows 183).
 constexpr uint64_t kWeightBlocks = 512, kWeightLeast = 128;
 
 // The entries (or rows) of a split: at least `least`, few enough that `units` of them give the blocks wanted, at
