@@ -85,8 +85,8 @@ struct Attn {
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float or_zero(float m) { return m == -kInf ? 0.0f : m; }
 
-// Where the partial results of row r of (sequence, kv head) lie: few rows of every pair (row_cap of
-// them), or, where sequences may have many, the tokens' own rows (row_cap 0).
+// Where the partial results of row r of (sequence, kv head) lie: row_cap rows of every pair, or, where
+// sequences may have many, the tokens' own rows (row_cap 0).
 __device__ __forceinline__ size_t part_row(const Attn& p, uint32_t split, uint32_t s, uint32_t h, int32_t t0, uint32_t r) {
   if (p.row_cap) return (((size_t)split * p.a.n_seq + s) * p.a.n_kv + h) * p.row_cap + r;
   return ((size_t)split * p.a.n_tok + (uint32_t)t0 + r / p.a.group) * p.a.n_q + h * p.a.group + r % p.a.group;
@@ -1006,7 +1006,7 @@ struct Plan {
   uint32_t few_rows;       // rows of a tile of the few-rows kernel: 16 or 32
   uint32_t few_most;       // rows of a pair up to which that kernel serves it; 0: none
   bool many;               // whether the many-rows kernel runs, for sequences of more rows
-  uint32_t few_chunk, few_split, few_cap, many_chunk, many_split, score_len;
+  uint32_t few_chunk, few_split, few_cap, many_chunk, many_split, many_cap, score_len;
   uint32_t w_split, w_rows, w_len;
   size_t o, ml, many_o, many_ml, scores, lse, part_w, keys, bytes;
 };
@@ -1117,8 +1117,11 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
   if (p.few_split > 1) p.o = take(p.few_split * few_part * a.dim * sizeof(float));
   if (p.few_split > 1 || (weights && !p.many)) p.ml = take(p.few_split * few_part * sizeof(float2));
   if (p.many && p.many_split > 1) {
-    p.many_o = take(p.many_split * all_rows * a.dim * sizeof(float));
-    p.many_ml = take(p.many_split * all_rows * sizeof(float2));
+    // token arrays may hold more rows than these sequences can have
+    p.many_cap = (uint64_t)a.n_seq * a.max_new < a.n_tok ? (uint32_t)row_most : 0;
+    const size_t many_part = p.many_cap ? pairs * p.many_cap : all_rows;
+    p.many_o = take(p.many_split * many_part * a.dim * sizeof(float));
+    p.many_ml = take(p.many_split * many_part * sizeof(float2));
   }
   if (weights && !p.many) {
     p.score_len = (uint32_t)up(a.max_len, 64);
@@ -1191,7 +1194,7 @@ hipError_t attend(const KvArgs& a, const KvRows& q, const Plan& plan, float scal
     p.part_ml = (float2*)(ws + plan.many_ml);
     p.n_split = plan.many_split;
     p.chunk = plan.many_chunk;
-    p.row_cap = 0;
+    p.row_cap = plan.many_cap;
     p.rows_from = plan.few_most;
     p.rows_to = row_most;
     hipLaunchKernelGGL((kv_many_kernel<M, D>),

@@ -271,6 +271,8 @@ def victims(pool, seqs, budget, first=0, recent=0, max_evict=1):
         for name, x in (("budget", budget), ("first", first), ("recent", recent), ("max_evict", max_evict)):
             if not 0 <= x < 1 << 31:
                 _refuse("%s out of range" % name)
+        if max_evict > 1 << 27:
+            _refuse("max_evict out of range")
         shape = (seqs.n_seq, pool.n_kv, max_evict)
         gone = torch.empty(shape, dtype=torch.int32, device=pool.device)
         src = torch.empty(shape, dtype=torch.int32, device=pool.device)

@@ -161,6 +161,23 @@ def test_strided_queries_and_rows_of_no_sequence(kv):
     K.near(kv.attend(pool, seqs, t, 0.1)[:3], want[:3], tol[:3], "out of transposed rows")
 
 
+@pytest.mark.parametrize("dim", [64, 256])
+@pytest.mark.parametrize("lens,new", [((1500,), (60,)), ((1500, 700), (60, 41))])
+def test_many_tokens_among_many_rows(kv, dim, lens, new):
+    """Rows of other calls in the same arrays: partial results are kept by sequence, not by row."""
+    import torch
+    c = K.Case("bf16", dim, 64, 1, 4, lens, new, tail=2000, seed=dim)
+    want, lse, _, tol, tol_lse, _ = c.attend(0.1)
+    pool, seqs = K.device(c)
+    n = sum(new)
+    for decay in (None, 0.5):
+        out = torch.full((c.n_tok, 4, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+        _, e = kv.attend(pool, seqs, K.rows(c.q, c.dtype), 0.1, decay=decay, lse=True, out=out)
+        assert (out[n:] == 7.0).all()
+        K.near(out[:n], want[:n], tol[:n], "out")
+        K.near(e[:n], lse[:n], tol_lse[:n], "lse")
+
+
 def test_bounds_of_the_device_arrays(kv):
     """Lengths and token ranges beyond the bounds are cut to them."""
     import torch

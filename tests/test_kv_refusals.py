@@ -125,6 +125,17 @@ def test_workspace_sizes(kv):
     assert n.value == 0
 
 
+@pytest.mark.parametrize("weights", [0, 1])
+def test_workspaces_go_by_the_tokens_that_sequences_can_have(kv, weights):
+    """One sequence of 64 new tokens among a million rows: its partial results, and a word a row and head."""
+    L, n = kv._kv(), C.c_size_t()
+    p = pool(kv, n_pages=5000, k=None, v=None)
+    s = seqs(kv, n_seq=1, max_pages=4000, max_new=64, n_tok=1 << 20, max_len=60000)
+    assert L.unison_kv_attend_size(C.byref(p), C.byref(s), 4, weights, 0, C.byref(n)) == OK
+    rows, splits, dim = 64 * 4, 60000 // 128, 256
+    assert n.value <= splits * rows * (dim + 2) * 4 + ((1 << 20) * 4 * 4 + 60256 * 4 * 64) * weights + 4096
+
+
 @pytest.mark.parametrize("n_sel,first,last", [(0, 0, 0), (4097, 0, 1), (2, 0, 0), (2, 1, 2), (4, 1 << 31, 1 << 31)])
 def test_block_counts(kv, n_sel, first, last):
     L = kv._kv()
