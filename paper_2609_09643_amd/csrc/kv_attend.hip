@@ -311,7 +311,8 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
   if (SCORES && p.score_lds && start < end) {  // everybody's scores are there: one run of memory
     f32x4* to = score_at(p, s, h, start >> 5, 0, 0);
     const uint32_t words = ((end - start + 63u) >> 6) * 16u * p.row_cap;
-    for (uint32_t x = tid; x < words; x += kBlock) to[x] = kept[x];
+    // past the caches, which keys and values pass through (the 64 sequences of kScoresLds: 566 us, through them 573)
+    for (uint32_t x = tid; x < words; x += kBlock) __builtin_nontemporal_store(kept[x], to + x);
   }
   if (wave) return;
   for (int n = 0; n < NT; ++n) {
