@@ -1091,10 +1091,11 @@ Plan plan_of(const KvArgs& a, bool weights, uint32_t n_sel) {
     p.keys = take((size_t)a.n_tok * a.n_kv * a.max_pages * sizeof(uint32_t));
   } else {
     // 17 to 32 rows: two row tiles leave the few-rows kernel fewer loads under way, but it needs no second pass
-    // for the weights and ends sooner where there is little to read.  (16 sequences of 8,192 entries, 8 heads,
-    // 8 tokens of 4 query heads: 142 us against 113 on the many-rows kernel; one of them 19 against 25; 13 of
-    // 5,003, one head of 256: 24 against 52; with weights 172 against 184, at 256 dimensions 251 against 212.)
-    const bool wide = a.dim >= 128 && pairs * a.max_len * a.dim * 4 >= 160000000ull && (!weights || a.dim == 256);
+    // for the weights and ends sooner where there is little to read.  (8 heads, 8 tokens of 4 query heads: 16
+    // sequences of 8,192 entries 142 us against 113 on the many-rows kernel, 4 of them 48 against 43 and with
+    // weights 66 against 59, one of them 20 on both; one head of 256, up to 5,003 entries: 13 sequences 24 against
+    // 30, 20 of them 38 against 35.)
+    const bool wide = a.dim >= 128 && pairs * a.max_len * a.dim * 4 >= 100000000ull;
     // Up to 16 rows: of 256 dimensions the few-rows kernel has two wavefronts' registers only (the same 16
     // sequences, one token each: 130 us against 113).
     p.few_most = !wide ? kRowsFew : a.dim == 256 && !weights ? 0 : 16;
