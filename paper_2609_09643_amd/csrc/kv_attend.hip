@@ -11,6 +11,9 @@
 // The softmax keeps a running maximum and sum in 32 bits.  The maximum is only moved when a score
 // passes it by kSlack (in powers of two), which a ballot tells: p then stays below 2^kSlack, and the
 // cross-lane maximum and the rescaling of the sums run a few times per row instead of once per tile.
+// In fp16 a p below 2^-25 would be rounded to 0, and thousands of weak entries with it that the sum counts.
+// Scores are therefore taken against the maximum less kLift there: a row's largest p lies in 2^7 .. 2^15
+// (the type ends at 2^16), and what is rounded away lies under 2^-32 of it.
 #include "kv_device.h"
 
 #include <type_traits>
@@ -29,6 +32,7 @@ typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 struct Bf16 {
   typedef __bf16 t;
   typedef b16x8 v8;
+  static constexpr float kLift = 0.0f;  // the exponents of 32 bits
   static __device__ __forceinline__ f32x4 mma16(v8 a, v8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -39,6 +43,7 @@ struct Bf16 {
 struct Fp16 {
   typedef _Float16 t;
   typedef h16x8 v8;
+  static constexpr float kLift = 7.0f;
   static __device__ __forceinline__ f32x4 mma16(v8 a, v8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
@@ -74,7 +79,7 @@ struct Attn {
   uint32_t n_sel;
   // Partial results of a split of the entries (part_row)
   float* part_o;        // [..][dim], times the exponential of the maximum
-  float2* part_ml;      // maximum (power of two) and sum
+  float2* part_ml;      // maximum (power of two, less kLift) and sum
   float* scores;        // of the dense few-rows kernel (score_at), or null
   uint32_t n_split, chunk, row_cap, score_len, score_lds;
   float* part_w;        // weights' sums of a split of the rows, [w_split][n_seq][n_kv][w_len]
@@ -258,10 +263,10 @@ __global__ __launch_bounds__(kBlock, NT * D <= 256 ? 2 : 1) void kv_few_kernel(A
         }
         for (int x = 0; x < 8; ++x) top = fmaxf(top, z[y][x]);
       }
-      if (__builtin_amdgcn_ballot_w64(top > m[n] + kSlack)) {
+      if (__builtin_amdgcn_ballot_w64(top > m[n] + (kSlack + M::kLift))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(m[n], top);
+        const float next = fmaxf(m[n], top - M::kLift);
         const float f = exp2_fast(m[n] - or_zero(next));
         m[n] = next;
         l[n] *= f;
@@ -655,10 +660,10 @@ __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_
     for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
     top *= scale;
     float f = 1.0f;
-    const bool moved = __builtin_amdgcn_ballot_w64(top > m + kSlack) != 0ull;
+    const bool moved = __builtin_amdgcn_ballot_w64(top > m + (kSlack + M::kLift)) != 0ull;
     if (moved) {
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(m, top);
+      const float next = fmaxf(m, top - M::kLift);
       f = exp2_fast(m - or_zero(next));
       m = next;
       l *= f;
