@@ -56,3 +56,50 @@ def test_long_weak_tails(kv, dim, n, new, group, max_pages, nats):
             + (np.maximum(2.0 ** -11 * p, 2.0 ** -32 * p.max()) + dp * p) @ np.abs(v[:limit])
     K.near(out, want, tol, "out")
     K.near(e, lse, tol_lse, "lse")
+
+
+def bounds(c, out, lse, scale, chosen=None):
+    """What the few-rows kernel's result may be off by: the result's own rounding, the scores', the exponentials' and
+    the sums' in 32 bits, and of p what its two parts leave: a rounding's half step of a half step."""
+    half = K.HALF[c.dtype]
+    tol = np.zeros_like(out)
+    for i in range(len(c.lens)):
+        for h in range(c.n_kv):
+            all_e, all_k, all_v = c.entries(i, h, c.lens[i])
+            for t, limit in c.rows(i):
+                use = all_e < limit
+                if chosen is not None:
+                    use &= np.isin(all_e // c.page, chosen[t, h])
+                k, v = all_k[use], np.abs(all_v[use])
+                if not len(k):
+                    continue
+                for x in range(h * c.group, (h + 1) * c.group):
+                    s = scale * (k @ c.q[t, x])
+                    p = np.exp(s - lse[t, x])
+                    ds = (c.dim + 2) * STEP * abs(scale) * (np.abs(k) @ np.abs(c.q[t, x])).max() \
+                        + 8 * STEP * (np.abs(s).max() + abs(lse[t, x]))
+                    dp = 2 * ds + (16 + len(k)) * STEP
+                    low = 2.0 ** -32 * p.max() if c.dtype == "fp16" else 0.0   # a part below the normal range
+                    tol[t, x] = half * np.abs(out[t, x]) + ((1.01 * half * half + dp) * p + low) @ v + 2.0 ** -25
+    return tol
+
+
+@pytest.mark.parametrize("dtype,dim,page,n_kv,group", [
+    ("bf16", 64, 16, 2, 3), ("bf16", 128, 64, 2, 4), ("fp16", 128, 32, 1, 5), ("bf16", 256, 32, 1, 6),
+    ("fp16", 256, 16, 1, 7), ("bf16", 64, 64, 1, 20), ("bf16", 256, 64, 1, 18)])
+@pytest.mark.parametrize("lens,new", [((9, 40), (1, 1)), ((300, 31, 700), (4, 1, 2))])
+def test_few_rows_keep_their_probabilities(kv, dtype, dim, page, n_kv, group, lens, new):
+    """Up to 32 rows a sequence and kv head: p is not rounded to the inputs' type."""
+    c = K.Case(dtype, dim, page, n_kv, group, lens, [min(n, 32 // group) for n in new], seed=dim + group)
+    scale = dim ** -0.5
+    want, lse, _, _, _, _ = c.attend(scale)
+    tol = bounds(c, want, lse, scale)
+    pool, seqs = K.device(c, max_len=max(lens))
+    q = K.rows(c.q, dtype)
+    K.near(kv.attend(pool, seqs, q, scale), want, tol, "out")
+    K.near(kv.attend(pool, seqs, q, scale, decay=1.0), want, tol, "out with weights")
+    sel = c.choose(4, 1, 2)
+    want, lse, _, _, _, _ = c.attend(scale, chosen=sel)
+    out, got = kv.attend_blocks(pool, seqs, q, 4, 1, 2, scale)
+    assert np.array_equal(got.cpu().numpy(), sel)
+    K.near(out, want, bounds(c, want, lse, scale, sel), "sparse out")
