@@ -486,7 +486,9 @@ typedef struct {
  * 2^(e-1) <= A < 2^e, the step is 2^(e-7) and the box holds floor(min / step)
  * and ceil(max / step) per dimension over the live keys, cut to -127..127
  * (step and box 0 for A < 2^-120).  Keys are finite where boxes are kept.
- * tok_pos: [n_tok], needed exactly when the pool has positions.
+ * tok_pos: [n_tok], needed exactly when the pool has positions.  What the call
+ * writes is no place that it reads: no new token's row or position, no entry
+ * of two sequences.
  * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
 int unison_kv_append(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
                      const unison_kv_rows* k, const unison_kv_rows* v, const int32_t* tok_pos);
@@ -512,9 +514,13 @@ int unison_kv_attend_size(const unison_kv_pool* pool, const unison_kv_seqs* seqs
  * workspace: at least unison_kv_attend_size() bytes, 256-byte aligned; its
  * contents mean nothing before and after the call; calls that may overlap
  * need workspaces of their own.
+ * out, lse and the workspace share no memory with each other, with q, the pool
+ * or the batch's arrays; only where no weights are kept may out be q itself,
+ * every row at the place of its own query.
  * Errors: UNISON_E_INVALID (also: weights without pool->weight, decay outside
  * 0..1, scale not finite, n_q no multiple of n_kv, over 128 query heads a kv
- * head, a short workspace), UNISON_E_CAPACITY, UNISON_E_HIP. */
+ * head, a short workspace, memory shared as above), UNISON_E_CAPACITY,
+ * UNISON_E_HIP. */
 int unison_kv_attend(void* hip_stream, void* workspace, size_t workspace_bytes,
                      const unison_kv_pool* pool, const unison_kv_seqs* seqs, uint32_t n_q,
                      const unison_kv_rows* q, float scale, int weights, float decay, void* out,
@@ -530,7 +536,8 @@ int unison_kv_attend(void* hip_stream, void* workspace, size_t workspace_bytes,
  * for the kv head's query heads, the largest magnitude in 64..127.  The sum is
  * a whole number, so the choice does not depend on an order of summation.
  * sel: [n_tok][n_kv][n_sel], the chosen ordinals ascending (pages[s][ordinal]),
- * -1 behind the last; rows of no sequence are left as they were.
+ * -1 behind the last; rows of no sequence are left as they were; its memory
+ * is shared with nothing else.
  * 1 <= last, first + last <= n_sel <= 4096, max_pages <= 32768 (else
  * UNISON_E_CAPACITY).  Needs the pool's boxes.  Weights are not kept.
  * Otherwise as unison_kv_attend. */

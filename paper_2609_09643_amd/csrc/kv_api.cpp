@@ -80,6 +80,54 @@ bool rows(const unison_kv_rows* r, KvRows& out) {
   return true;
 }
 
+struct Span {
+  uintptr_t at;
+  uint64_t bytes;
+};
+
+Span span(const void* p, uint64_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), p ? bytes : 0}; }
+
+bool meet(const Span& x, const Span& y) {
+  return x.bytes && y.bytes && x.at < y.at + y.bytes && y.at < x.at + x.bytes;
+}
+
+// Whether one of the `n` written spans shares memory with another, with the pool or with the batch's arrays.
+bool overlaps(const KvArgs& a, const Span* written, int n) {
+  const uint64_t words = (uint64_t)a.n_pages * a.n_kv * a.page, boxes = (uint64_t)a.n_pages * a.n_kv;
+  const Span read[] = {span(a.k, words * a.dim * 2), span(a.v, words * a.dim * 2), span(a.weight, words * 4),
+                       span(a.pos, words * 4), span(a.box, boxes * 2 * a.dim), span(a.box_scale, boxes * 4),
+                       span(a.pages, (uint64_t)a.n_seq * a.max_pages * 4), span(a.len, (uint64_t)a.n_seq * 4),
+                       span(a.tok, ((uint64_t)a.n_seq + 1) * 4)};
+  for (int i = 0; i < n; ++i) {
+    for (const Span& r : read)
+      if (meet(written[i], r)) return true;
+    for (int j = 0; j < i; ++j)
+      if (meet(written[i], written[j])) return true;
+  }
+  return false;
+}
+
+// The same for a written span and the query rows.  Strides may leave room between these, so where the span lies
+// inside their extent the rows are looked at one by one.
+bool meets_rows(const KvArgs& a, const KvRows& q, const Span& w) {
+  typedef unsigned __int128 u128;
+  const u128 head = (u128)(a.n_q - 1) * q.head + a.dim, all = (u128)(a.n_tok - 1) * q.tok + head;
+  if (all >> 56) return true;  // no memory holds such rows
+  const auto rows = [&](uint64_t at, uint64_t elements) { return span((const char*)q.p + 2 * at, 2 * elements); };
+  if (!meet(w, rows(0, (uint64_t)all))) return false;
+  for (uint64_t t = 0; t < a.n_tok; ++t) {
+    if (!meet(w, rows(t * q.tok, (uint64_t)head))) continue;
+    for (uint64_t h = 0; h < a.n_q; ++h)
+      if (meet(w, rows(t * q.tok + h * q.head, a.dim))) return true;
+  }
+  return false;
+}
+
+// Whether the results are the query rows themselves, each over its own.
+bool in_place(const KvArgs& a, const KvRows& q, const void* out) {
+  return out == q.p && (a.n_tok == 1 || q.tok == (uint64_t)a.n_q * a.dim) && (a.n_q == 1 || q.head == a.dim);
+}
+
 int heads(KvArgs& a, uint32_t n_q) {
   if (n_q < 1 || n_q % a.n_kv || n_q / a.n_kv > kMaxGroup) return UNISON_E_INVALID;
   a.n_q = n_q;
@@ -107,6 +155,14 @@ int attend(void* hip_stream, void* ws, size_t ws_bytes, const unison_kv_pool* po
   if (!kv_attend_fits(a, n_sel)) return UNISON_E_CAPACITY;
   const size_t need = kv_attend_bytes(a, weights != 0, n_sel);
   if (need && (ws_bytes < need || !on(ws, 256))) return UNISON_E_INVALID;
+  const uint64_t tok_rows = (uint64_t)a.n_tok * n_q;
+  const Span written[] = {span(out, tok_rows * a.dim * 2), span(lse, tok_rows * 4), span(ws, need),
+                          span(sel, (uint64_t)a.n_tok * a.n_kv * n_sel * 4)};
+  if (overlaps(a, written, 4)) return UNISON_E_INVALID;
+  // a block without weights has its query rows in registers before it writes their results; the weights' second
+  // product reads them again
+  for (const Span& w : written)
+    if (meets_rows(a, r, w) && !(&w == written && !weights && in_place(a, r, out))) return UNISON_E_INVALID;
   return done(launch_kv_attend(a, r, scale, weights != 0, decay, n_sel, first, last, out, lse, sel, ws,
                                reinterpret_cast<hipStream_t>(hip_stream)));
 }

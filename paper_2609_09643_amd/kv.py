@@ -224,7 +224,8 @@ def _scale(scale, pool):
 def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
     """Attention of the new tokens q [n_tok, n_q, head_dim] over their sequences; scale: default
     1 / sqrt(head_dim).  decay: pool.weight becomes decay * weight + the tokens' attention weights
-    (None: it stays).  Returns out, or (out, lse [n_tok, n_q]) with lse = True."""
+    (None: it stays).  out: a tensor for the result, whose memory may be q's own (out = q) only where
+    decay is None.  Returns out, or (out, lse [n_tok, n_q]) with lse = True."""
     torch = _torch()
     with _On(pool, seqs) as stream:
         r = _rows(q, "q", pool, seqs.n_tok, None)
