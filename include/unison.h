@@ -559,8 +559,10 @@ int unison_kv_attend_blocks(void* hip_stream, void* workspace, size_t workspace_
  *                                and past new_len, ascending; else -1
  * Nothing in the pool changes.  Needs the pool's weights and positions;
  * budget >= first + recent, budget >= 1, 1 <= max_evict <= 2^27.  The three
- * arrays are 4-byte aligned.
- * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
+ * arrays are 4-byte aligned and share no memory with each other, the pool or
+ * the batch's arrays (new_len is not len).
+ * Errors: UNISON_E_INVALID (also: memory shared so), UNISON_E_CAPACITY,
+ * UNISON_E_HIP. */
 int unison_kv_victims(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
                       uint32_t budget, uint32_t first, uint32_t recent, uint32_t max_evict,
                       int32_t* victims, int32_t* src, int32_t* new_len);

@@ -226,6 +226,11 @@ int unison_kv_victims(void* hip_stream, const unison_kv_pool* pool, const unison
   rc = pointers(a, false);
   if (rc != UNISON_OK) return rc;
   if (!a.weight || !a.pos || !on(victims, 4) || !on(src, 4) || !on(new_len, 4)) return UNISON_E_INVALID;
+  // the lengths among what is read: a block of one head writes new_len while the other heads' read len
+  const uint64_t list = (uint64_t)a.n_seq * a.n_kv * max_evict * 4;
+  const Span written[] = {span(victims, list), span(src, list), span(new_len, (uint64_t)a.n_seq * 4)};
+  a.tok = nullptr;  // not looked at
+  if (overlaps(a, written, 3)) return UNISON_E_INVALID;
   return done(launch_kv_victims(a, budget, first, recent, max_evict, victims, src, new_len,
                                 reinterpret_cast<hipStream_t>(hip_stream)));
 }

@@ -126,3 +126,27 @@ def test_results_between_the_rows(host):
 def test_each_refusal_by_itself(host, weights, blocks, change):
     """The checks of the arguments, each with nothing else wrong."""
     assert attend(host, weights, blocks, **change) == INVALID
+
+
+def test_eviction_lists_stand_apart(host):
+    """The lengths among them: one head's block would write them while another's reads them."""
+    kv, lib = host
+
+    def victims(**move):
+        at = dict(AT, **move)
+        p, s, _ = (C.byref(x) for x in structs(kv, at))
+        return lib.unison_kv_victims(None, p, s, 8, 0, 0, EVICT, at["victims"], at["src"], at["new_len"])
+
+    assert victims() == OK
+    assert victims(new_len=AT["len"]) == INVALID
+    assert victims(new_len=AT["tok"]) == OK                        # token ranges are not read here
+    written = ["victims", "src", "new_len"]
+    for w in written:
+        for other in written + ["weight", "pos", "pages", "len"]:
+            if other == w:
+                continue
+            end = AT[other] + BYTES[other]
+            assert victims(**{w: end - 4}) == INVALID, (w, other)
+            assert victims(**{w: end}) == OK, (w, other, "behind")
+            assert victims(**{w: AT[other] - BYTES[w]}) == OK, (w, other, "before")
+            assert victims(**{w: AT[other] - BYTES[w] + 4}) == INVALID, (w, other)
