@@ -6,7 +6,8 @@ are the calls of include/unison.h with the same meaning.  Every call runs on
 the current stream of the tensors' device and allocates its outputs and its
 workspace with torch, so calls on several streams or in several captured
 graphs do not share memory.  The tensors behind a Pool and a Seqs stay where
-they are: lengths and page tables are updated in place.
+they are: lengths and page tables are updated in place.  There is no backward
+pass: tensors that autograd follows are refused.
 """
 from __future__ import annotations
 
@@ -86,6 +87,20 @@ def _need(t, name, dtype, shape, device):
             name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
+_dual = None
+
+
+def _no_history(t, name):
+    """The operators have no backward pass: what autograd follows is refused rather than dropped."""
+    global _dual
+    if _dual is None:
+        from torch.autograd.forward_ad import unpack_dual as _dual
+    if t.requires_grad and _torch().is_grad_enabled():
+        _refuse("%s requires a gradient, and there is no backward pass: detach it, or call under torch.no_grad()" % name)
+    if _dual(t).tangent is not None:
+        _refuse("%s has a tangent, and there is no forward-mode derivative" % name)
+
+
 class Pool:
     """Pages of a KV pool: k [n_pages, n_kv, page, head_dim], v [n_pages, n_kv, head_dim, page] in
     bfloat16 or float16; weight (float32) and pos (int32) [n_pages, n_kv, page]; box (int8)
@@ -108,6 +123,9 @@ class Pool:
         if box is not None:
             _need(box, "box", torch.int8, (n_pages, n_kv, 2, dim), k.device)
             _need(box_scale, "box_scale", torch.float32, (n_pages, n_kv), k.device)
+        self._floats = tuple(t for t in (k, v, weight) if t is not None)
+        for t in self._floats:
+            _no_history(t, "the pool")
         self.k, self.v, self.weight, self.pos, self.box, self.box_scale = k, v, weight, pos, box, box_scale
         self.n_kv, self.page, self.head_dim, self.dtype, self.device = n_kv, page, dim, k.dtype, k.device
         ptr = lambda t: None if t is None else t.data_ptr()
@@ -163,6 +181,9 @@ class _On:
     def __init__(self, pool, seqs):
         if seqs.device != pool.device:
             _refuse("the sequences are on %s, the pool on %s" % (seqs.device, pool.device))
+        for t in pool._floats:
+            if t.requires_grad:  # set after the pool was made
+                _no_history(t, "the pool")
         self.device = pool.device
 
     def __enter__(self):
@@ -185,6 +206,7 @@ def _rows(t, name, pool, n_tok, heads):
             t.shape[2] != pool.head_dim or (heads is not None and t.shape[1] != heads):
         _refuse("%s: %s [%d, heads, %d] on %s wanted, got %s %s on %s" % (
             name, pool.dtype, n_tok, pool.head_dim, pool.device, t.dtype, tuple(t.shape), t.device))
+    _no_history(t, name)
     s = t.stride()
     if s[2] != 1 or s[0] < 0 or s[1] < 0:
         _refuse("%s: the head dimension has to be contiguous" % name)
@@ -234,6 +256,7 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
             out = torch.empty((seqs.n_tok, n_q, pool.head_dim), dtype=pool.dtype, device=pool.device)
         else:
             _need(out, "out", pool.dtype, (seqs.n_tok, n_q, pool.head_dim), pool.device)
+            _no_history(out, "out")
         e = torch.empty((seqs.n_tok, n_q), dtype=torch.float32, device=pool.device) if lse else None
         n, ws = _workspace(pool, seqs, n_q, int(decay is not None), 0)
         _check(_kv().unison_kv_attend(stream, None if ws is None else ws.data_ptr(), n, pool._ref, seqs._ref, n_q,
