@@ -59,9 +59,14 @@ def _kv():
     return _lib
 
 
+_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _module
+    if _module is None:
+        import torch as _module
+    return _module
 
 
 _raw = None
@@ -77,12 +82,23 @@ def _raw_stream(index):
     return _raw(index)
 
 
+_count = 0
+
+
+def _several():
+    """Whether there is more than one device, of which another may be the current one."""
+    global _count
+    if not _count:
+        _count = _torch().cuda.device_count()
+    return _count > 1
+
+
 def _refuse(why):
     raise UnisonError(E_INVALID, why)
 
 
 def _need(t, name, dtype, shape, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         _refuse("%s: contiguous %s %s on %s wanted, got %s %s on %s" % (
             name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
@@ -99,6 +115,18 @@ def _no_history(t, name):
         _refuse("%s requires a gradient, and there is no backward pass: detach it, or call under torch.no_grad()" % name)
     if _dual(t).tangent is not None:
         _refuse("%s has a tangent, and there is no forward-mode derivative" % name)
+
+
+_bump = None
+
+
+def _wrote(tensors):
+    """Tells autograd that a kernel changed these tensors in place, so that a backward pass that saved their old
+    values fails instead of using the new ones."""
+    global _bump
+    if _bump is None:
+        from torch.autograd.graph import increment_version as _bump
+    _bump(tensors)
 
 
 class Pool:
@@ -124,11 +152,13 @@ class Pool:
             _need(box, "box", torch.int8, (n_pages, n_kv, 2, dim), k.device)
             _need(box_scale, "box_scale", torch.float32, (n_pages, n_kv), k.device)
         self._floats = tuple(t for t in (k, v, weight) if t is not None)
+        self._entries = tuple(t for t in (k, v, weight, pos, box, box_scale) if t is not None)
         for t in self._floats:
             _no_history(t, "the pool")
         self.k, self.v, self.weight, self.pos, self.box, self.box_scale = k, v, weight, pos, box, box_scale
         self.n_kv, self.page, self.head_dim, self.dtype, self.device = n_kv, page, dim, k.dtype, k.device
         ptr = lambda t: None if t is None else t.data_ptr()
+        self._index = k.device.index if k.device.type == "cuda" else None
         self._args = PoolArgs(BF16 if k.dtype == torch.bfloat16 else FP16, dim, n_kv, page, n_pages, 0, ptr(k), ptr(v),
                               ptr(weight), ptr(pos), ptr(box), ptr(box_scale))
         self._ref = C.byref(self._args)
@@ -176,42 +206,45 @@ class Seqs:
 class _On:
     """The device of a call made current, and its stream."""
 
-    __slots__ = ("device", "before")
+    __slots__ = ("index", "before")
 
     def __init__(self, pool, seqs):
         if seqs.device != pool.device:
             _refuse("the sequences are on %s, the pool on %s" % (seqs.device, pool.device))
-        for t in pool._floats:
-            if t.requires_grad:  # set after the pool was made
+        if pool.k.requires_grad or pool.v.requires_grad or (pool.weight is not None and pool.weight.requires_grad):
+            for t in pool._floats:  # set after the pool was made
                 _no_history(t, "the pool")
-        self.device = pool.device
+        self.index = pool._index
 
     def __enter__(self):
-        torch = _torch()
-        if self.device.type != "cuda":
-            _refuse("the operators run on the GPU, the pool is on %s" % self.device)
-        index = self.device.index
-        self.before = torch.cuda.current_device()
-        if self.before != index:
-            torch.cuda.set_device(index)
+        index = self.index
+        if index is None:
+            _refuse("the operators run on the GPU, the pool is on another device")
+        self.before = index
+        if _several():
+            cuda = _torch().cuda
+            self.before = cuda.current_device()
+            if self.before != index:
+                cuda.set_device(index)
         return _raw_stream(index)
 
     def __exit__(self, *exc):
-        if self.before != self.device.index:
+        if self.before != self.index:
             _torch().cuda.set_device(self.before)
 
 
 def _rows(t, name, pool, n_tok, heads):
-    if t.dim() != 3 or t.dtype != pool.dtype or t.device != pool.device or t.shape[0] != n_tok or \
-            t.shape[2] != pool.head_dim or (heads is not None and t.shape[1] != heads):
+    shape = t.shape
+    if len(shape) != 3 or t.dtype != pool.dtype or t.device != pool.device or shape[0] != n_tok or \
+            shape[2] != pool.head_dim or (heads is not None and shape[1] != heads):
         _refuse("%s: %s [%d, heads, %d] on %s wanted, got %s %s on %s" % (
-            name, pool.dtype, n_tok, pool.head_dim, pool.device, t.dtype, tuple(t.shape), t.device))
+            name, pool.dtype, n_tok, pool.head_dim, pool.device, t.dtype, tuple(shape), t.device))
     _no_history(t, name)
-    s = t.stride()
-    if s[2] != 1 or s[0] < 0 or s[1] < 0:
+    tok, head, element = t.stride()
+    if element != 1 or tok < 0 or head < 0:
         _refuse("%s: the head dimension has to be contiguous" % name)
     # the stride of a single row or head is never walked
-    return RowsArgs(t.data_ptr(), s[0] if t.shape[0] > 1 else 0, s[1] if t.shape[1] > 1 else 0)
+    return RowsArgs(t.data_ptr(), tok if n_tok > 1 else 0, head if shape[1] > 1 else 0)
 
 
 def _int32(t, name, shape, device):
@@ -227,6 +260,7 @@ def append(pool, seqs, k, v, positions=None):
         rk, rv = _rows(k, "k", pool, seqs.n_tok, pool.n_kv), _rows(v, "v", pool, seqs.n_tok, pool.n_kv)
         pos = None if positions is None else _int32(positions, "positions", (seqs.n_tok,), pool.device)
         _check(_kv().unison_kv_append(stream, pool._ref, seqs._ref, C.byref(rk), C.byref(rv), pos))
+        _wrote(pool._entries)
 
 
 def _workspace(pool, seqs, n_q, weights, n_sel):
@@ -251,7 +285,7 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
     torch = _torch()
     with _On(pool, seqs) as stream:
         r = _rows(q, "q", pool, seqs.n_tok, None)
-        n_q = q.shape[1]
+        n_q, given = q.shape[1], out is not None
         if out is None:
             out = torch.empty((seqs.n_tok, n_q, pool.head_dim), dtype=pool.dtype, device=pool.device)
         else:
@@ -262,6 +296,10 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
         _check(_kv().unison_kv_attend(stream, None if ws is None else ws.data_ptr(), n, pool._ref, seqs._ref, n_q,
                                       C.byref(r), _scale(scale, pool), int(decay is not None), decay or 0.0,
                                       out.data_ptr(), None if e is None else e.data_ptr()))
+        if given:
+            _wrote(out)
+        if decay is not None:
+            _wrote(pool.weight)
     return (out, e) if lse else out
 
 
@@ -315,3 +353,4 @@ def compact(pool, seqs, victims, src, new_len):
         v, s = _int32(victims, "victims", shape, pool.device), _int32(src, "src", shape, pool.device)
         n = _int32(new_len, "new_len", (seqs.n_seq,), pool.device)
         _check(_kv().unison_kv_compact(stream, pool._ref, seqs._ref, shape[2], v, s, n))
+        _wrote(pool._entries)
