@@ -532,9 +532,10 @@ int unison_kv_attend(void* hip_stream, void* workspace, size_t workspace_bytes,
  * ones of highest score, ties to the lower page:
  *   score = step * sum over the kv head's query heads and dimensions of
  *           max(qi * lower, qi * upper)
- * with qi the query rounded to whole steps (half to even) of one power of two
- * for the kv head's query heads, the largest magnitude in 64..127.  The sum is
- * a whole number, so the choice does not depend on an order of summation.
+ * with qi the query, negated where scale is negative, rounded to whole steps
+ * (half to even) of one power of two for the kv head's query heads, the largest
+ * magnitude in 64..127.  The sum is a whole number, so the choice does not
+ * depend on an order of summation; it is taken to 24 bits, as is the product.
  * sel: [n_tok][n_kv][n_sel], the chosen ordinals ascending (pages[s][ordinal]),
  * -1 behind the last; rows of no sequence are left as they were; its memory
  * is shared with nothing else.

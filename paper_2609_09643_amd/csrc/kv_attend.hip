@@ -1243,15 +1243,16 @@ bool kv_attend_fits(const KvArgs& a, uint32_t n_sel) {
   return (uint64_t)a.n_kv * p.many_split <= most && rows / many_rows(a.dim) < 65535;
 }
 
-hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, uint32_t n_sel, uint32_t first, uint32_t last,
-                            uint32_t* keys, int32_t* sel, hipStream_t st);
+hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, bool negate, uint32_t n_sel, uint32_t first,
+                            uint32_t last, uint32_t* keys, int32_t* sel, hipStream_t st);
 
 hipError_t launch_kv_attend(const KvArgs& a, const KvRows& q, float scale, bool weights, float decay,
                             uint32_t n_sel, uint32_t first, uint32_t last, void* out, float* lse, int32_t* sel,
                             void* ws, hipStream_t st) {
   const Plan plan = plan_of(a, weights, n_sel);
   if (n_sel) {
-    const hipError_t rc = launch_kv_choose(a, q, n_sel, first, last, (uint32_t*)((char*)ws + plan.keys), sel, st);
+    const hipError_t rc =
+        launch_kv_choose(a, q, scale < 0.0f, n_sel, first, last, (uint32_t*)((char*)ws + plan.keys), sel, st);
     if (rc != hipSuccess) return rc;
   }
   const auto run = [&](auto m, auto d) {

@@ -734,8 +734,8 @@ constexpr uint32_t kScorePages = 64;  // of a block, 16 a wavefront
 // 7-bit halves, so that the products are byte dot products.  Bound by latency and the boxes' bytes: 2,047 pages,
 // 8 heads of 128: 5.4 us; 24 sequences of up to 512 pages and 2 tokens: 12.5 us (32 MB of boxes).
 template <typename T, int D>
-__global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, uint32_t first, uint32_t last,
-                                                          uint32_t* keys) {
+__global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, bool negate, uint32_t first,
+                                                          uint32_t last, uint32_t* keys) {
   constexpr uint32_t LP = 2 * D / 16, PP = 64 / LP;  // lanes of a page, pages of a wavefront's load
   __shared__ alignas(16) uint8_t half[2][2 * D];     // low and high 7 bits: D of the lower side, D of the upper
   __shared__ float lds[kBlock / 64];
@@ -759,7 +759,7 @@ __global__ __launch_bounds__(kBlock) void kv_score_kernel(KvArgs a, KvRows nq, u
   if ((tid & 63u) == 0u) lds[tid >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
-  const float inv = kv_step(top).inv;
+  const float inv = negate ? -kv_step(top).inv : kv_step(top).inv;  // a negative scale prefers the smallest q.k
   if (tid < D) {
     int32_t n = 0, p = 0;
     for (uint32_t g = 0; g < a.group; ++g) {
@@ -916,13 +916,13 @@ hipError_t launch_kv_compact(const KvArgs& a, uint32_t max_evict, const int32_t*
   });
 }
 
-hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, uint32_t n_sel, uint32_t first, uint32_t last,
-                            uint32_t* keys, int32_t* sel, hipStream_t st) {
+hipError_t launch_kv_choose(const KvArgs& a, const KvRows& q, bool negate, uint32_t n_sel, uint32_t first,
+                            uint32_t last, uint32_t* keys, int32_t* sel, hipStream_t st) {
   const uint32_t pages = (a.max_len + a.page - 1) / a.page;
   const dim3 grid(a.max_new * ((pages + kScorePages - 1) / kScorePages), a.n_kv, a.n_seq);
   const hipError_t rc = with_type(a, [&](auto t, auto d) {
-    hipLaunchKernelGGL((kv_score_kernel<decltype(t), decltype(d)::value>), grid, dim3(kBlock), 0, st, a, q, first, last,
-                       keys);
+    hipLaunchKernelGGL((kv_score_kernel<decltype(t), decltype(d)::value>), grid, dim3(kBlock), 0, st, a, q, negate,
+                       first, last, keys);
   });
   if (rc != hipSuccess) return rc;
   const bool fits = with_pick(pages, [&](auto block, auto per) {
