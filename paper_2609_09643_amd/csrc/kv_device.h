@@ -79,15 +79,6 @@ __host__ __device__ __forceinline__ size_t kv_word(const KvArgs& a, int32_t page
   return ((size_t)page * a.n_kv + h) * a.page;
 }
 
-__device__ __forceinline__ float to_f32(__hip_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ __hip_bfloat16 from_f32<__hip_bfloat16>(float x) { return __float2bfloat16(x); }
-template <>
-__device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half(x); }
-
 // A power of two that brings a largest magnitude `top` into [64, 128), and its inverse; both 0 for
 // magnitudes below 2^-120.  Multiplying by either is exact, so the int8 images and the scores made
 // from them are the same whoever computes them.
