@@ -481,7 +481,7 @@ __device__ __forceinline__ float magnitude(float scale2) { return fmaxf(fabsf(sc
 // two are put side by side: while the exponentials of a group of 32 entries run, the matrix cores do
 // the second product of the group before and the first product of the group behind.
 // 4 sequences of up to 2,000 tokens over up to 12,001 entries, 32 query and 8 kv heads of 128 (928 GFLOP seen):
-// 890 us, 1.04 PFLOP/s; a large library product reaches 1.38.  Its matrix cores are busy 54 % of the time, its
+// 900 us, 1.03 PFLOP/s; a large library product reaches 1.38.  Its matrix cores are busy 54 % of the time, its
 // vector units 41 %.  Four tiles in LDS in place of two, their loads awaited by number, took 2 to 5 % longer.
 template <typename M, int D>
 __global__ __launch_bounds__(64 * many_waves(D), D <= 128 ? 2 : 1) void kv_many_kernel(Attn p) {

@@ -339,8 +339,8 @@ __device__ __forceinline__ Bits<PER> pick_chosen(const uint32_t (&key)[PER], Cut
 constexpr uint32_t kFewVictims = 4;
 
 // One block per (kv head, sequence) of up to BLOCK * PER entries: weights and positions are read once into
-// registers (twice of more than 32 a thread).  Bound by latency, that of its chain of loads and barriers: 8
-// sequences of up to 32,768 entries and 8 heads (64 blocks) down to 8,192: 40 us for 25 MB.
+// registers (twice of more than 32 a thread).  Bound by vector instructions (busy 65 to 71 % of the time) and the
+// barriers between them: 8 sequences of up to 32,768 entries and 8 heads (64 blocks) down to 8,192: 39 us for 25 MB.
 template <int BLOCK, int PER>
 __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvArgs a, uint32_t budget, uint32_t first,
                                                            uint32_t recent, uint32_t max_evict,
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(BLOCK, PER <= 8 ? 8 : 4) void kv_victims_kernel(KvA
 }
 
 // Longer sequences than a block's registers hold are read again in every pass (8 of up to 66,000 entries:
-// 390 us; of 60,000 in registers 87).
+// 420 us; of 65,536 in registers 89).
 constexpr uint32_t kSelBlock = 1024;
 
 // Inclusive sum over the block of a word per thread; `total` is the block's.

@@ -281,7 +281,8 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
     """Attention of the new tokens q [n_tok, n_q, head_dim] over their sequences; scale: default
     1 / sqrt(head_dim).  decay: pool.weight becomes decay * weight + the tokens' attention weights
     (None: it stays).  out: a tensor for the result, whose memory may be q's own (out = q) only where
-    decay is None.  Returns out, or (out, lse [n_tok, n_q]) with lse = True."""
+    decay is None.  Returns out, or (out, lse [n_tok, n_q]) with lse = True; rows that belong to no
+    sequence are not written: in tensors made here they hold anything."""
     torch = _torch()
     with _On(pool, seqs) as stream:
         r = _rows(q, "q", pool, seqs.n_tok, None)
@@ -305,7 +306,8 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
 
 def attend_blocks(pool, seqs, q, n_sel, first=0, last=1, scale=None, lse=False):
     """The same over at most n_sel pages a token and kv head: the first and the last of those it sees
-    and the ones of highest box score.  Returns (out, sel int32 [n_tok, n_kv, n_sel]) and lse."""
+    and the ones of highest box score.  Returns (out, sel int32 [n_tok, n_kv, n_sel]) and lse, whose
+    rows that belong to no sequence hold anything."""
     torch = _torch()
     with _On(pool, seqs) as stream:
         r = _rows(q, "q", pool, seqs.n_tok, None)
