@@ -486,9 +486,9 @@ typedef struct {
  * 2^(e-1) <= A < 2^e, the step is 2^(e-7) and the box holds floor(min / step)
  * and ceil(max / step) per dimension over the live keys, cut to -127..127
  * (step and box 0 for A < 2^-120).  Keys are finite where boxes are kept.
- * tok_pos: [n_tok], needed exactly when the pool has positions.  What the call
- * writes is no place that it reads: no new token's row or position, no entry
- * of two sequences.
+ * tok_pos: [n_tok], needed exactly when the pool has positions.  The new
+ * tokens' rows and positions lie where the call does not write, and no entry
+ * that it writes belongs to two sequences.
  * Errors: UNISON_E_INVALID, UNISON_E_CAPACITY, UNISON_E_HIP. */
 int unison_kv_append(void* hip_stream, const unison_kv_pool* pool, const unison_kv_seqs* seqs,
                      const unison_kv_rows* k, const unison_kv_rows* v, const int32_t* tok_pos);

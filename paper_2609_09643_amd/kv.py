@@ -106,13 +106,16 @@ def _need(t, name, dtype, shape, device):
 _dual = None
 
 
-def _no_history(t, name):
+def _no_gradient(t, name):
     """The operators have no backward pass: what autograd follows is refused rather than dropped."""
+    if t.requires_grad and _torch().is_grad_enabled():
+        _refuse("%s requires a gradient, and there is no backward pass: detach it, or call under torch.no_grad()" % name)
+
+
+def _no_tangent(t, name):
     global _dual
     if _dual is None:
         from torch.autograd.forward_ad import unpack_dual as _dual
-    if t.requires_grad and _torch().is_grad_enabled():
-        _refuse("%s requires a gradient, and there is no backward pass: detach it, or call under torch.no_grad()" % name)
     if _dual(t).tangent is not None:
         _refuse("%s has a tangent, and there is no forward-mode derivative" % name)
 
@@ -154,7 +157,7 @@ class Pool:
         self._floats = tuple(t for t in (k, v, weight) if t is not None)
         self._entries = tuple(t for t in (k, v, weight, pos, box, box_scale) if t is not None)
         for t in self._floats:
-            _no_history(t, "the pool")
+            _no_tangent(t, "the pool")
         self.k, self.v, self.weight, self.pos, self.box, self.box_scale = k, v, weight, pos, box, box_scale
         self.n_kv, self.page, self.head_dim, self.dtype, self.device = n_kv, page, dim, k.dtype, k.device
         ptr = lambda t: None if t is None else t.data_ptr()
@@ -208,12 +211,14 @@ class _On:
 
     __slots__ = ("index", "before")
 
-    def __init__(self, pool, seqs):
+    def __init__(self, pool, seqs, whole=False):
+        """whole: a call whose results are whole numbers, which have no gradient."""
         if seqs.device != pool.device:
             _refuse("the sequences are on %s, the pool on %s" % (seqs.device, pool.device))
-        if pool.k.requires_grad or pool.v.requires_grad or (pool.weight is not None and pool.weight.requires_grad):
-            for t in pool._floats:  # set after the pool was made
-                _no_history(t, "the pool")
+        if not whole and (pool.k.requires_grad or pool.v.requires_grad or
+                          (pool.weight is not None and pool.weight.requires_grad)):
+            for t in pool._floats:
+                _no_gradient(t, "the pool")
         self.index = pool._index
 
     def __enter__(self):
@@ -239,7 +244,8 @@ def _rows(t, name, pool, n_tok, heads):
             shape[2] != pool.head_dim or (heads is not None and shape[1] != heads):
         _refuse("%s: %s [%d, heads, %d] on %s wanted, got %s %s on %s" % (
             name, pool.dtype, n_tok, pool.head_dim, pool.device, t.dtype, tuple(shape), t.device))
-    _no_history(t, name)
+    _no_gradient(t, name)
+    _no_tangent(t, name)
     tok, head, element = t.stride()
     if element != 1 or tok < 0 or head < 0:
         _refuse("%s: the head dimension has to be contiguous" % name)
@@ -291,7 +297,8 @@ def attend(pool, seqs, q, scale=None, decay=None, lse=False, out=None):
             out = torch.empty((seqs.n_tok, n_q, pool.head_dim), dtype=pool.dtype, device=pool.device)
         else:
             _need(out, "out", pool.dtype, (seqs.n_tok, n_q, pool.head_dim), pool.device)
-            _no_history(out, "out")
+            _no_gradient(out, "out")
+            _no_tangent(out, "out")
         e = torch.empty((seqs.n_tok, n_q), dtype=torch.float32, device=pool.device) if lse else None
         n, ws = _workspace(pool, seqs, n_q, int(decay is not None), 0)
         _check(_kv().unison_kv_attend(stream, None if ws is None else ws.data_ptr(), n, pool._ref, seqs._ref, n_q,
@@ -331,7 +338,7 @@ def victims(pool, seqs, budget, first=0, recent=0, max_evict=1):
     """The entries that leave sequences of more than `budget`, by least weight: (victims, src, new_len),
     int32 [n_seq, n_kv, max_evict] twice and [n_seq]."""
     torch = _torch()
-    with _On(pool, seqs) as stream:
+    with _On(pool, seqs, whole=True) as stream:
         for name, x in (("budget", budget), ("first", first), ("recent", recent), ("max_evict", max_evict)):
             if not 0 <= x < 1 << 31:
                 _refuse("%s out of range" % name)

@@ -51,21 +51,22 @@ def test_rows_with_a_tangent(kv):
 
 
 @pytest.mark.parametrize("name", ["k", "v", "weight"])
-def test_pools_that_require_a_gradient(kv, name):
-    t = tensors()
-    t[name].requires_grad_()
-    with pytest.raises(UnisonError, match="gradient"):
-        kv.Pool(**t)
-    with torch.no_grad():
-        kv.Pool(**t)
-
-
-@pytest.mark.parametrize("name", ["k", "v", "weight"])
-def test_pools_that_come_to_require_a_gradient(kv, name):
-    pool, seqs = kv.Pool(**tensors()), batch(kv)
-    kv._On(pool, seqs)
-    getattr(pool, name).requires_grad_()
-    with pytest.raises(UnisonError, match="gradient"):
+@pytest.mark.parametrize("before", [False, True])
+def test_pools_that_require_a_gradient(kv, name, before):
+    """From the start (the parameters of a module that runs without gradients) or later on: the calls refuse."""
+    t, seqs = tensors(), batch(kv)
+    if before:
+        t[name].requires_grad_()
+    pool = kv.Pool(**t)
+    if not before:
         kv._On(pool, seqs)
-    with torch.no_grad():
-        kv._On(pool, seqs)
+        t[name].requires_grad_()
+    for call in (lambda: kv.attend(pool, seqs, torch.zeros(2, 4, 64, dtype=torch.bfloat16)),
+                 lambda: kv.attend_blocks(pool, seqs, torch.zeros(2, 4, 64, dtype=torch.bfloat16), 1),
+                 lambda: kv.append(pool, seqs, t["k"], t["v"]), lambda: kv.compact(pool, seqs, None, None, None)):
+        with pytest.raises(UnisonError, match="gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(UnisonError, match="GPU"):
+            call()
+    with pytest.raises(UnisonError, match="GPU"):                       # whole numbers have no gradient
+        kv.victims(pool, seqs, 4)
